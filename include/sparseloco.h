@@ -351,6 +351,114 @@ int sl_rice_encode(sl_plan *plan, const void *payload, void *out, size_t out_cap
                    void *workspace, void *stream);
 int sl_rice_decode(sl_plan *plan, const void *in, size_t in_bytes, void *payload, void *stream);
 
+/* ---- The inner step: what a worker computes between two outer steps (Algorithm 1, inner
+ * loop: AdamW with the gradient clipped to a global norm), on the same flat arenas.
+ *
+ * Types of dense inputs and outputs */
+enum { SL_TYPE_F32 = 0, SL_TYPE_BF16 = 1 };
+
+/* AdamW over a list of tensors, all of them in one launch.  The list is given as to
+ * sl_plan_create; `layout` has no effect here, tensors may be of any size, and there is no k.
+ * `decay`: host array, a factor on the weight decay for every tensor (0 = none), copied;
+ * NULL = 1 for all.  At most 2^24 - 1 runs of 4096 elements (each tensor's own, the last one
+ * short) in the whole list.  Allocates small device tables on the current device (freed by sl_adamw_destroy). */
+typedef struct sl_adamw sl_adamw;
+int sl_adamw_create(const sl_tensor *tensors, int n_tensors, const float *decay, sl_adamw **out);
+int sl_adamw_destroy(sl_adamw *opt);
+/* Blocks of 256 consecutive elements that share a scale in the 8-bit states: those of a tensor
+ * begin with it, its last one may be short; numbered tensor by tensor. */
+int64_t sl_adamw_num_blocks(const sl_adamw *opt);
+size_t sl_grad_norm_workspace_bytes(const sl_adamw *opt);
+
+/* Norm of all gradients of the list and the factor that clips it:
+ *   result[0] = sqrt(sum over all elements of grad^2)      (fp64 sums in a fixed order)
+ *   result[1] = max_norm / norm where norm > max_norm, else 1; NaN where the norm is infinite
+ *               or NaN.  A step that is given result + 1 as its grad_scale then clips, and
+ *               leaves everything as it is where a gradient was not finite.
+ * grad      in,  device, arena of grad_type, 16-byte aligned
+ * max_norm  > 0 (infinity: no clipping)
+ * result    out, device, float[2];  workspace: device, 256-byte aligned */
+int sl_grad_norm(sl_adamw *opt, const void *grad, int grad_type, float max_norm, float *result, void *workspace,
+                 void *stream);
+
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;
+    int64_t step;            /* 1 for the first */
+} sl_adamw_params;
+
+/* One AdamW step.  Per element, every product, sum, quotient and root rounded to fp32 on its own:
+ *   g = grad_scale * grad                            (g = grad where grad_scale is NULL)
+ *   m <- m*beta1 + g*(1 - beta1) ;  v <- v*beta2 + (g*g)*(1 - beta2)
+ *   theta <- theta*(1 - decay*(lr*weight_decay)) - (m*(lr/(1 - beta1^step))) / (sqrt(v)*r + eps),
+ *   r = 1/sqrt(1 - beta2^step); constants are formed in fp64 and rounded once.
+ * theta, m, v  inout, device, fp32 arenas, 16-byte aligned, distinct
+ * grad         in, device, arena of grad_type, 16-byte aligned
+ * grad_scale   in, device, one float, or NULL; if it is NaN nothing is written at all
+ * theta16      out, device, or NULL: a bf16 arena that receives theta rounded to nearest
+ * 0 <= beta1, beta2 < 1, eps > 0, step >= 1, all finite, else INVALID_ARG. */
+int sl_adamw_step(sl_adamw *opt, float *theta, const void *grad, int grad_type, float *m, float *v,
+                  const sl_adamw_params *params, const float *grad_scale, void *theta16, void *stream);
+
+/* The same step with both moments held in 8 bits: theta is computed from the moments that were
+ * stored, brought up to date in fp32, which are then stored again.
+ *   codes   device, one byte per element, at the element's place in an arena of bytes, 16-byte aligned
+ *   scales  device, one byte X per block: the block's values are multiples of 2^(X - 127);
+ *           X = 255: every value of the block is NaN; zeros are moments of zero
+ *   m       sign, 4 bits of exponent, 3 of mantissa: up to 1.875 * 2^(X-127), down to 2^-17 of it
+ *   v       5 bits of exponent, 3 of mantissa: the same, down to 2^-33 * 2^(X-127); a positive v is never
+ *           stored as zero (the next step would divide by it)
+ * X is the smallest with every value of the block <= 1.875 * 2^(X-127) (at most 253: larger ones are
+ * cut off there).  Values are rounded up or down at random, in proportion to the distance: rounded to
+ * nearest, a v that changes by less than half a code's step would never change at all.  The random
+ * bits of an element are h = fmix32(fmix32(fmix32(seed) ^ block) ^ place in block), the low 16 for m,
+ * the high 16 for v (fmix32: see sl_compress_random_k); a caller takes a fresh seed every step.
+ * Everything else as sl_adamw_step. */
+int sl_adamw_step8(sl_adamw *opt, float *theta, const void *grad, int grad_type, uint8_t *m_codes, uint8_t *v_codes,
+                   uint8_t *m_scales, uint8_t *v_scales, uint32_t seed, const sl_adamw_params *params,
+                   const float *grad_scale, void *theta16, void *stream);
+/* The values that 8-bit states stand for (moment 1 = m, 2 = v): `values` out, device, fp32 arena. */
+int sl_adamw_state_values(sl_adamw *opt, int moment, const uint8_t *codes, const uint8_t *scales, float *values,
+                          void *stream);
+
+/* ---- Linear layers on microscaled 4-bit operands.
+ *
+ * A matrix of rows x cols is held as elements of 4 bits (E2M1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
+ * negatives) and one scale byte X (a factor 2^(X - 127), 255 = NaN) for every 32 consecutive elements
+ * of a row, the last block of a row possibly short.  X is the smallest with every element of the block
+ * <= 6 * 2^(X-127) - none is cut off; elements are rounded to nearest, ties to the even code.  A block with
+ * an infinity or a NaN has X = 255 and is NaN as a whole.
+ * In memory: the codes in tiles of 16 rows x 128 columns, row tile by row tile - in a tile, block
+ * b = 0..3 of row r is the 16 bytes at 256*b + 16*r, element 2i in the low half of byte i; then the scales
+ * in tiles of 64 rows x 128 columns - the byte of block b of row r is at 64*b + 4*(r mod 16) + r/16.
+ * Rows and columns that fill up tiles are zero.  sl_mx4_bytes() is the size (0 for a size that is not
+ * positive or has more than 2^25 tiles of codes); 16-byte aligned. */
+size_t sl_mx4_bytes(int64_t rows, int64_t cols);
+
+/* src     in,  device, rows x cols of src_type, row r at element r*ld (ld >= cols), aligned to its element
+ * q       out, device, sl_mx4_bytes(rows, cols): blocks along the rows, or NULL
+ * qt      out, device, sl_mx4_bytes(cols, rows): the transposed matrix, blocks along src's columns, or
+ *         NULL; at least one of the two.  Both come from one pass over src. */
+int sl_mx4_quantize(const void *src, int src_type, int64_t rows, int64_t cols, int64_t ld, void *q, void *qt,
+                    void *stream);
+/* The values of q, each rounded once where the type is bf16 and its exponent is out of range. */
+int sl_mx4_dequantize(const void *q, int64_t rows, int64_t cols, void *out, int out_type, int64_t ld, void *stream);
+
+/* c[i][j] = sum over l of a[i][l] * b[j][l]  (+ c[i][j] where accumulate is not 0), a of m x k, b of n x k:
+ * exact products, fp32 sums in an order that depends on the sizes alone, rounded once for bf16.
+ *   y  = x W^T   product(x, w)          dx = dy W   product(dy, w^T)          dW = dy^T x   product(dy^T, x^T)
+ * with w^T, dy^T, x^T the qt of sl_mx4_quantize.
+ * c          device, m x n of c_type, row i at element i*ldc (ldc >= n), aligned to its element
+ * accumulate only with SL_TYPE_F32
+ * m, n >= 0, m*n <= 2^36; k >= 0 (k = 0: sums of nothing; a and b are not read)
+ * workspace  device, sl_mx4_workspace_bytes(m, n, k), 16-byte aligned; may be NULL where that is 0 */
+size_t sl_mx4_workspace_bytes(int64_t m, int64_t n, int64_t k);
+int sl_mx4_product(const void *a, const void *b, int64_t m, int64_t n, int64_t k, void *c, int c_type, int64_t ldc,
+                   int accumulate, void *workspace, void *stream);
+/* y = Q(x) w^T for a dense x (m x k of x_type, row i at element i*ldx): sl_mx4_quantize of x and
+ * sl_mx4_product in one call; for a few rows (generation, one token per sequence) in one launch. */
+int sl_mx4_linear(const void *x, int x_type, int64_t ldx, const void *w, int64_t m, int64_t n, int64_t k, void *y,
+                  int y_type, int64_t ldy, void *workspace, void *stream);
+
 /* Per-kernel timing for benchmarks.  Between sl_profile_begin and
  * sl_profile_end every sl_compress / sl_decompress_avg_apply call on the plan
  * records HIP events on its stream around each of its kernels (no

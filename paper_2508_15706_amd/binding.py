@@ -35,6 +35,9 @@ EXPORTS = [
     "sl_lom_direction", "sl_dense_avg_apply", "sl_decompress_avg_apply_nesterov", "sl_sub_topk",
     "sl_compress_random_k", "sl_compress_noalloc", "sl_plan_set_codes_wave_below", "sl_coded_fixed_bytes",
     "sl_compress_coded", "sl_decompress_avg_apply_coded", "sl_decompress_avg_apply_nesterov_coded",
+    "sl_adamw_create", "sl_adamw_destroy", "sl_adamw_num_blocks", "sl_grad_norm_workspace_bytes", "sl_grad_norm",
+    "sl_adamw_step", "sl_adamw_step8", "sl_adamw_state_values",
+    "sl_mx4_bytes", "sl_mx4_quantize", "sl_mx4_dequantize", "sl_mx4_workspace_bytes", "sl_mx4_product", "sl_mx4_linear",
 ]
 PROF_PHASES = ["select", "stats", "codes", "lut", "residual", "apply", "index"]
 
@@ -42,6 +45,11 @@ PROF_PHASES = ["select", "stats", "codes", "lut", "residual", "apply", "index"]
 class SlTensor(C.Structure):
     _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("offset", C.c_int64),
                 ("layout", C.c_int32), ("reserved", C.c_int32)]
+
+
+class SlAdamwParams(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("weight_decay", C.c_double), ("step", C.c_int64)]
 
 
 class SparseLoCoError(RuntimeError):
@@ -130,6 +138,35 @@ def lib():
         L.sl_profile_begin.argtypes = [vp, i32]
         L.sl_profile_end.restype = i32
         L.sl_profile_end.argtypes = [vp, C.POINTER(C.c_double), C.POINTER(i32)]
+        pf, pp = C.POINTER(C.c_float), C.POINTER(SlAdamwParams)
+        L.sl_adamw_create.restype = i32
+        L.sl_adamw_create.argtypes = [C.POINTER(SlTensor), i32, pf, C.POINTER(vp)]
+        L.sl_adamw_destroy.restype = i32
+        L.sl_adamw_destroy.argtypes = [vp]
+        L.sl_adamw_num_blocks.restype = i64
+        L.sl_adamw_num_blocks.argtypes = [vp]
+        L.sl_grad_norm_workspace_bytes.restype = sz
+        L.sl_grad_norm_workspace_bytes.argtypes = [vp]
+        L.sl_grad_norm.restype = i32
+        L.sl_grad_norm.argtypes = [vp, vp, i32, C.c_float, vp, vp, vp]
+        L.sl_adamw_step.restype = i32
+        L.sl_adamw_step.argtypes = [vp, vp, vp, i32, vp, vp, pp, vp, vp, vp]
+        L.sl_adamw_step8.restype = i32
+        L.sl_adamw_step8.argtypes = [vp, vp, vp, i32, vp, vp, vp, vp, C.c_uint32, pp, vp, vp, vp]
+        L.sl_adamw_state_values.restype = i32
+        L.sl_adamw_state_values.argtypes = [vp, i32, vp, vp, vp, vp]
+        L.sl_mx4_bytes.restype = sz
+        L.sl_mx4_bytes.argtypes = [i64, i64]
+        L.sl_mx4_quantize.restype = i32
+        L.sl_mx4_quantize.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp]
+        L.sl_mx4_dequantize.restype = i32
+        L.sl_mx4_dequantize.argtypes = [vp, i64, i64, vp, i32, i64, vp]
+        L.sl_mx4_workspace_bytes.restype = sz
+        L.sl_mx4_workspace_bytes.argtypes = [i64, i64, i64]
+        L.sl_mx4_product.restype = i32
+        L.sl_mx4_product.argtypes = [vp, vp, i64, i64, i64, vp, i32, i64, i32, vp, vp]
+        L.sl_mx4_linear.restype = i32
+        L.sl_mx4_linear.argtypes = [vp, i32, i64, vp, i64, i64, i64, vp, i32, i64, vp, vp]
         L.sl_strerror.restype = C.c_char_p
         L.sl_strerror.argtypes = [i32]
         L.sl_last_hip_error.restype = C.c_char_p
@@ -456,3 +493,170 @@ def sl_payload_validate(plan: Plan, payload: torch.Tensor, workspace: torch.Tens
     if st:
         raise SparseLoCoError("sl_payload_validate", st)
     return True
+
+
+# ---- the inner step ----
+
+_TYPES = {torch.float32: 0, torch.bfloat16: 1}            # SL_TYPE_F32, SL_TYPE_BF16
+
+
+def _type_of(t: torch.Tensor) -> int:
+    if t.dtype not in _TYPES:
+        raise ValueError(f"expected float32 or bfloat16, got {t.dtype}")
+    return _TYPES[t.dtype]
+
+
+def _matrix(t: torch.Tensor):
+    """(pointer, type, rows, cols, row stride) of a device matrix whose rows are contiguous."""
+    if not t.is_cuda or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("expected a device matrix with contiguous rows")
+    rows, cols = t.shape
+    return t.data_ptr(), _type_of(t), rows, cols, (t.stride(0) if rows > 1 else max(cols, t.stride(0)))
+
+
+def _mx4_ptr(q: Optional[torch.Tensor], rows: int, cols: int) -> Optional[int]:
+    if q is not None and q.numel() < sl_mx4_bytes(rows, cols):
+        raise ValueError(f"a 4-bit matrix of {rows} x {cols} has {sl_mx4_bytes(rows, cols)} bytes, got {q.numel()}")
+    return _dev_ptr(q, torch.uint8)
+
+
+class AdamW:
+    """Owner of an sl_adamw handle."""
+
+    def __init__(self, handle: int, n_tensors: int):
+        self.handle, self.n_tensors = handle, n_tensors
+
+    @property
+    def num_blocks(self) -> int:
+        return int(lib().sl_adamw_num_blocks(self.handle))
+
+    def close(self):
+        if self.handle:
+            lib().sl_adamw_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def sl_adamw_create(descs: Sequence[Sequence[int]], decay: Optional[Sequence[float]] = None) -> AdamW:
+    """descs: (rows, cols, offset, layout) per tensor; decay: a factor on the weight decay per tensor."""
+    descs = list(descs)
+    arr = (SlTensor * max(1, len(descs)))()
+    for i, (r, c, off, lay) in enumerate(descs):
+        arr[i] = SlTensor(int(r), int(c), int(off), int(lay), 0)
+    if decay is not None and len(decay) != len(descs):
+        raise ValueError("one decay factor per tensor")
+    factors = None if decay is None else (C.c_float * max(1, len(descs)))(*[float(d) for d in decay])
+    h = C.c_void_p()
+    st = lib().sl_adamw_create(arr, len(descs), factors, C.byref(h))
+    if st:
+        raise SparseLoCoError("sl_adamw_create", st)
+    return AdamW(h.value, len(descs))
+
+
+def alloc_norm_workspace(opt: AdamW, device="cuda") -> torch.Tensor:
+    return torch.empty(int(lib().sl_grad_norm_workspace_bytes(opt.handle)), dtype=torch.uint8, device=device)
+
+
+def sl_grad_norm(opt: AdamW, grad: torch.Tensor, max_norm: float, result: torch.Tensor, workspace: torch.Tensor,
+                 stream=None) -> None:
+    """result: two fp32 values, the norm and the factor that clips it (grad_scale of a step: result[1:])."""
+    st = lib().sl_grad_norm(opt.handle, _dev_ptr(grad), _type_of(grad), float(max_norm),
+                            _dev_ptr(result, torch.float32), _dev_ptr(workspace, torch.uint8), _stream_ptr(stream))
+    if st:
+        raise SparseLoCoError("sl_grad_norm", st)
+
+
+def sl_adamw_step(opt: AdamW, theta: torch.Tensor, grad: torch.Tensor, m: torch.Tensor, v: torch.Tensor, lr: float,
+                  beta1: float, beta2: float, eps: float, weight_decay: float, step: int,
+                  grad_scale: Optional[torch.Tensor] = None, theta16: Optional[torch.Tensor] = None, stream=None) -> None:
+    params = SlAdamwParams(lr, beta1, beta2, eps, weight_decay, step)
+    st = lib().sl_adamw_step(opt.handle, _dev_ptr(theta, torch.float32), _dev_ptr(grad), _type_of(grad),
+                             _dev_ptr(m, torch.float32), _dev_ptr(v, torch.float32), C.byref(params),
+                             _dev_ptr(grad_scale, torch.float32), _dev_ptr(theta16, torch.bfloat16), _stream_ptr(stream))
+    if st:
+        raise SparseLoCoError("sl_adamw_step", st)
+
+
+def sl_adamw_step8(opt: AdamW, theta: torch.Tensor, grad: torch.Tensor, m_codes: torch.Tensor, v_codes: torch.Tensor,
+                   m_scales: torch.Tensor, v_scales: torch.Tensor, seed: int, lr: float, beta1: float, beta2: float,
+                   eps: float, weight_decay: float, step: int, grad_scale: Optional[torch.Tensor] = None,
+                   theta16: Optional[torch.Tensor] = None, stream=None) -> None:
+    params = SlAdamwParams(lr, beta1, beta2, eps, weight_decay, step)
+    st = lib().sl_adamw_step8(opt.handle, _dev_ptr(theta, torch.float32), _dev_ptr(grad), _type_of(grad),
+                              _dev_ptr(m_codes, torch.uint8), _dev_ptr(v_codes, torch.uint8),
+                              _dev_ptr(m_scales, torch.uint8), _dev_ptr(v_scales, torch.uint8), int(seed) & 0xFFFFFFFF,
+                              C.byref(params), _dev_ptr(grad_scale, torch.float32), _dev_ptr(theta16, torch.bfloat16),
+                              _stream_ptr(stream))
+    if st:
+        raise SparseLoCoError("sl_adamw_step8", st)
+
+
+def sl_adamw_state_values(opt: AdamW, moment: int, codes: torch.Tensor, scales: torch.Tensor, values: torch.Tensor,
+                          stream=None) -> None:
+    st = lib().sl_adamw_state_values(opt.handle, int(moment), _dev_ptr(codes, torch.uint8), _dev_ptr(scales, torch.uint8),
+                                     _dev_ptr(values, torch.float32), _stream_ptr(stream))
+    if st:
+        raise SparseLoCoError("sl_adamw_state_values", st)
+
+
+def sl_mx4_bytes(rows: int, cols: int) -> int:
+    return int(lib().sl_mx4_bytes(int(rows), int(cols)))
+
+
+def alloc_mx4(rows: int, cols: int, device="cuda") -> torch.Tensor:
+    return torch.empty(max(16, sl_mx4_bytes(rows, cols)), dtype=torch.uint8, device=device)
+
+
+def sl_mx4_workspace_bytes(m: int, n: int, k: int) -> int:
+    return int(lib().sl_mx4_workspace_bytes(int(m), int(n), int(k)))
+
+
+def alloc_mx4_workspace(m: int, n: int, k: int, device="cuda") -> torch.Tensor:
+    return torch.empty(max(16, sl_mx4_workspace_bytes(m, n, k)), dtype=torch.uint8, device=device)
+
+
+def sl_mx4_quantize(src: torch.Tensor, q: Optional[torch.Tensor], qt: Optional[torch.Tensor] = None, stream=None) -> None:
+    p, typ, rows, cols, ld = _matrix(src)
+    st = lib().sl_mx4_quantize(p, typ, rows, cols, ld, _mx4_ptr(q, rows, cols), _mx4_ptr(qt, cols, rows), _stream_ptr(stream))
+    if st:
+        raise SparseLoCoError("sl_mx4_quantize", st)
+
+
+def sl_mx4_dequantize(q: torch.Tensor, out: torch.Tensor, stream=None) -> None:
+    p, typ, rows, cols, ld = _matrix(out)
+    st = lib().sl_mx4_dequantize(_mx4_ptr(q, rows, cols), rows, cols, p, typ, ld, _stream_ptr(stream))
+    if st:
+        raise SparseLoCoError("sl_mx4_dequantize", st)
+
+
+def sl_mx4_product(a: torch.Tensor, b: torch.Tensor, c: torch.Tensor, k: int, workspace: Optional[torch.Tensor] = None,
+                   accumulate: bool = False, stream=None) -> None:
+    """c (m x n) = a b^T for a of m x k and b of n x k, both in 4 bits."""
+    p, typ, m, n, ld = _matrix(c)
+    if workspace is not None and workspace.numel() < sl_mx4_workspace_bytes(m, n, k):
+        raise ValueError("workspace too small")
+    pa, pb = (_mx4_ptr(a, m, k), _mx4_ptr(b, n, k)) if m and n else (None, None)       # (nothing to do: nothing is read)
+    st = lib().sl_mx4_product(pa, pb, m, n, int(k), p, typ, ld, int(accumulate),
+                              _dev_ptr(workspace, torch.uint8), _stream_ptr(stream))
+    if st:
+        raise SparseLoCoError("sl_mx4_product", st)
+
+
+def sl_mx4_linear(x: torch.Tensor, w: torch.Tensor, y: torch.Tensor, workspace: Optional[torch.Tensor] = None,
+                  stream=None) -> None:
+    """y (m x n) = Q(x) w^T for a dense x (m x k) and w (n x k) in 4 bits."""
+    xp, xt, m, k, ldx = _matrix(x)
+    yp, yt, rows, n, ldy = _matrix(y)
+    if rows != m:
+        raise ValueError("x and y have different numbers of rows")
+    if workspace is not None and workspace.numel() < sl_mx4_workspace_bytes(m, n, k):
+        raise ValueError("workspace too small")
+    st = lib().sl_mx4_linear(xp, xt, ldx, _mx4_ptr(w, n, k), m, n, k, yp, yt, ldy, _dev_ptr(workspace, torch.uint8),
+                             _stream_ptr(stream))
+    if st:
+        raise SparseLoCoError("sl_mx4_linear", st)
