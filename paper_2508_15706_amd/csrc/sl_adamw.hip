@@ -10,6 +10,7 @@
 
 #include "sl_device.h"
 #include "sl_internal.h"
+#include "sl_mx4.h"
 
 namespace {
 
@@ -57,26 +58,18 @@ SL_DEV sl_f4 load_grad(const void *arena, long long p, int n)
     }
 }
 
-// fp32 to bf16, to nearest, ties to even; NaN stays NaN.
-SL_DEV unsigned bf16_bits(float x)
-{
-    const unsigned b = __float_as_uint(x);
-    if ((b & 0x7FFFFFFFu) > 0x7F800000u) return (b >> 16) | 0x40u;
-    return (b + 0x7FFFu + ((b >> 16) & 1u)) >> 16;
-}
-
 SL_DEV void store_bf16(unsigned short *p, int n, sl_f4 v)
 {
     if (n >= 4) {
         typedef unsigned u2 __attribute__((ext_vector_type(2)));
         u2 w;
-        w.x = bf16_bits(v.x) | bf16_bits(v.y) << 16;
-        w.y = bf16_bits(v.z) | bf16_bits(v.w) << 16;
+        w.x = sl_bf16_pair(v.x, v.y);
+        w.y = sl_bf16_pair(v.z, v.w);
         __builtin_nontemporal_store(w, reinterpret_cast<u2 *>(p));
     } else {
 #pragma unroll
         for (int c = 0; c < 4; ++c)
-            if (c < n) p[c] = (unsigned short)bf16_bits(v[c]);
+            if (c < n) p[c] = (unsigned short)sl_bf16_bits(v[c]);
     }
 }
 

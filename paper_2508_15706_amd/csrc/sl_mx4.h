@@ -48,43 +48,103 @@ SL_DEV float sl_mx4_factor(unsigned x)
     return __uint_as_float(x == 0u ? 0x400000u : x == 255u ? 0x7FC00000u : x << 23);
 }
 
-// 32 elements to 16 bytes (the conversion divides by the factor, rounds to nearest even and cuts off above 6).
-SL_DEV sl_u4 sl_mx4_pack(const float (&v)[32], unsigned x)
+// Two elements to the byte SEL of a word (divided by the factor, to nearest even, cut off above 6).
+template <int SEL>
+SL_DEV unsigned sl_mx4_pair(unsigned old, float a, float b, float factor)
 {
-    sl_u4 w = {0, 0, 0, 0};
-    if (x == 255u) return w;
-    const float f = sl_mx4_factor(x);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        unsigned o = 0;
-        o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, v[8 * i + 0], v[8 * i + 1], f, 0);
-        o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, v[8 * i + 2], v[8 * i + 3], f, 1);
-        o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, v[8 * i + 4], v[8 * i + 5], f, 2);
-        o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, v[8 * i + 6], v[8 * i + 7], f, 3);
-        w[i] = o;
-    }
-    return w;
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(old, a, b, factor, SEL);
+}
+typedef __bf16 sl_bf2 __attribute__((ext_vector_type(2)));
+template <int SEL>
+SL_DEV unsigned sl_mx4_pair(unsigned old, unsigned bf16_pair, float factor)
+{
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(old, __builtin_bit_cast(sl_bf2, bf16_pair), factor, SEL);
 }
 
-SL_DEV unsigned sl_mx4_top(const float (&v)[32])
+// The same of a pair of bf16: each half's magnitude.
+SL_DEV unsigned sl_pair_max(unsigned a, unsigned b)
 {
-    unsigned top = 0;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-    return top;
+    typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(us2, a), __builtin_bit_cast(us2, b)));
 }
 
+// Eight consecutive elements of a dense matrix as they lie in memory, of which the first n exist (n <= 0: none); the
+// others are zero.  The address is aligned to the element only, which a 16-byte access of this target may be.
 template <bool B16>
-SL_DEV float sl_dense_at(const void *p, long long i)
+struct SlOctet {
+    unsigned w[B16 ? 4 : 8];
+
+    SL_DEV void load(const void *src, long long at, int n)
+    {
+        typedef unsigned u4a __attribute__((ext_vector_type(4), aligned(2)));
+#pragma unroll
+        for (int i = 0; i < (B16 ? 4 : 8); ++i) w[i] = 0;
+        if constexpr (B16) {
+            const unsigned short *p = static_cast<const unsigned short *>(src) + at;
+            if (n >= 8) {
+                const sl_u4 v = __builtin_nontemporal_load(reinterpret_cast<const u4a *>(p));
+                w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 7; ++i)
+                    if (i < n) w[i >> 1] |= (unsigned)p[i] << (16 * (i & 1));
+            }
+        } else {
+            const unsigned *p = static_cast<const unsigned *>(src) + at;
+            if (n >= 8) {
+                const sl_u4 u = __builtin_nontemporal_load(reinterpret_cast<const u4a *>(p));
+                const sl_u4 v = __builtin_nontemporal_load(reinterpret_cast<const u4a *>(p + 4));
+                w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w, w[4] = v.x, w[5] = v.y, w[6] = v.z, w[7] = v.w;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 7; ++i)
+                    if (i < n) w[i] = p[i];
+            }
+        }
+    }
+    // fp32 bits of the largest magnitude
+    SL_DEV unsigned top() const
+    {
+        if constexpr (B16) {
+            unsigned t = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t = sl_pair_max(t, w[i] & 0x7FFF7FFFu);
+            return max(t << 16, t & 0xFFFF0000u);
+        } else {
+            unsigned t = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t = max(t, w[i] & 0x7FFFFFFFu);
+            return t;
+        }
+    }
+    SL_DEV unsigned pack(unsigned x) const
+    {
+        const float f = sl_mx4_factor(x);
+        unsigned o = 0;
+        if constexpr (B16) {
+            o = sl_mx4_pair<0>(o, w[0], f), o = sl_mx4_pair<1>(o, w[1], f);
+            o = sl_mx4_pair<2>(o, w[2], f), o = sl_mx4_pair<3>(o, w[3], f);
+        } else {
+            o = sl_mx4_pair<0>(o, __uint_as_float(w[0]), __uint_as_float(w[1]), f);
+            o = sl_mx4_pair<1>(o, __uint_as_float(w[2]), __uint_as_float(w[3]), f);
+            o = sl_mx4_pair<2>(o, __uint_as_float(w[4]), __uint_as_float(w[5]), f);
+            o = sl_mx4_pair<3>(o, __uint_as_float(w[6]), __uint_as_float(w[7]), f);
+        }
+        return x == 255u ? 0u : o;
+    }
+};
+
+// Maximum over the four lanes of a quad.
+SL_DEV unsigned sl_quad_max(unsigned v)
 {
-    if constexpr (B16) return __uint_as_float((unsigned)static_cast<const unsigned short *>(p)[i] << 16);
-    else return static_cast<const float *>(p)[i];
+    v = max(v, (unsigned)sl_dpp<SL_DPP_XOR1>((int)v));
+    return max(v, (unsigned)sl_dpp<SL_DPP_XOR2>((int)v));
 }
 
-// fp32 to bf16, to nearest, ties to even; NaN stays NaN.
-SL_DEV unsigned sl_bf16_bits(float x)
+// fp32 to bf16, to nearest, ties to even (the conversion instruction of this target).
+SL_DEV unsigned sl_bf16_bits(float x) { return (unsigned)__builtin_bit_cast(unsigned short, (__bf16)x); }
+SL_DEV unsigned sl_bf16_pair(float a, float b)
 {
-    const unsigned b = __float_as_uint(x);
-    if ((b & 0x7FFFFFFFu) > 0x7F800000u) return (b >> 16) | 0x40u;
-    return (b + 0x7FFFu + ((b >> 16) & 1u)) >> 16;
+    const sl_bf2 v = {(__bf16)a, (__bf16)b};
+    return __builtin_bit_cast(unsigned, v);
 }

@@ -6,57 +6,163 @@ namespace {
 
 struct QuantArgs {
     const void *src;
-    long long rows, cols, ld;        // of src
-    unsigned char *q;
-    long long row_tiles, col_tiles, scales;   // of q
-    long long groups;                // row tiles and what fills up the last scale tile
+    long long rows, cols, ld;
+    unsigned char *q, *qt;
+    SlMx4Shape s, t;                 // of q and of qt
+    long long col_groups;            // workgroups in a row of them
 };
 
-// A wave per tile of 16 rows x 128 columns of q: lane l has block l / 16 of row l % 16 to itself.  T: q is the
-// transposed matrix, its rows are src's columns.
-template <bool B16, bool T>
+// A workgroup takes 128 columns of 128 (bf16) or 64 (fp32) rows, eight consecutive elements of a row in a lane at a
+// time, 16 rows per access.
+//
+// Along the rows (Q) a block is a quad of lanes: its largest magnitude comes by two lane moves, its codes are one word
+// a lane, and the 256 threads' words of an access are one tile of codes, 1 KB.  A block's scale byte and those of the
+// same block 16, 32 and 48 rows on are the word that the first lane of the quad writes.
+// Along the columns (QT) the elements pass through LDS as they are; a lane then has 32 rows of two columns (bf16, one
+// wave for each block of 32 rows) or of one (fp32, two waves), read row by row without bank conflicts.
+template <bool B16, bool Q, bool QT>
 __global__ void __launch_bounds__(256) k_quantize(QuantArgs A)
 {
-    const int lane = threadIdx.x & 63, wave = sl_uniform((int)(threadIdx.x >> 6));
-    const long long tile = (long long)blockIdx.x * 4 + wave;
-    if (tile >= A.groups * A.col_tiles) return;
-    const long long rt = tile / A.col_tiles, kt = tile % A.col_tiles;
-    const long long row = rt * MX_ROWS + (lane & 15), col = kt * MX_COLS + (lane >> 4) * MX_BLOCK;
-    const long long n_rows = T ? A.cols : A.rows, n_cols = T ? A.rows : A.cols;
-    float v[32];
+    constexpr int ROWS = B16 ? 128 : 64, WORDS = B16 ? 4 : 8;
+    __shared__ sl_u4 tile[QT ? ROWS * 16 * WORDS / 4 : 1];
+    const int tid = threadIdx.x, octet = tid & 15, sub = tid >> 4;
+    const long long rg = blockIdx.x / A.col_groups, kt = blockIdx.x % A.col_groups;
+    const long long row0 = rg * ROWS, col = kt * MX_COLS + octet * 8;
+    const int n = (int)max(min(A.cols - col, 8ll), 0ll);
+    SlOctet<B16> v[ROWS / 16];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        v[i] = 0.0f;
-        if (row < n_rows && col + i < n_cols) v[i] = sl_dense_at<B16>(A.src, T ? (col + i) * A.ld + row : row * A.ld + col + i);
+    for (int i = 0; i < ROWS / 16; ++i) {
+        const long long row = row0 + i * 16 + sub;
+        v[i].load(A.src, row * A.ld + col, row < A.rows ? n : 0);
     }
-    const unsigned x = sl_mx4_scale(sl_mx4_top(v));
-    if (rt < A.row_tiles)
-        *reinterpret_cast<sl_u4 *>(A.q + tile * MX_TILE_BYTES + lane * 16) = sl_mx4_pack(v, x);
-    A.q[A.scales + ((rt >> 2) * A.col_tiles + kt) * MX_SCALE_TILE_BYTES + lane * 4 + (rt & 3)] = (unsigned char)x;
+    if constexpr (QT) {
+#pragma unroll
+        for (int i = 0; i < ROWS / 16; ++i)
+#pragma unroll
+            for (int j = 0; j < WORDS / 4; ++j)
+                tile[((i * 16 + sub) * 16 + octet) * (WORDS / 4) + j] = sl_u4{v[i].w[4 * j], v[i].w[4 * j + 1], v[i].w[4 * j + 2], v[i].w[4 * j + 3]};
+    }
+    if constexpr (Q) {
+        const int b = octet >> 2;
+#pragma unroll
+        for (int i = 0; i < ROWS / 16; i += 4) {
+            const long long rt = row0 / 16 + i;
+            unsigned scales = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const unsigned x = sl_mx4_scale(sl_quad_max(v[i + j].top()));
+                scales |= x << (8 * j);
+                const unsigned w = v[i + j].pack(x);
+                if (rt + j < A.s.row_tiles)
+                    *reinterpret_cast<unsigned *>(A.q + ((rt + j) * A.s.col_tiles + kt) * MX_TILE_BYTES + b * 256 + sub * 16 + (octet & 3) * 4) = w;
+            }
+            if ((octet & 3) == 0 && rt < A.s.row_tiles)
+                *reinterpret_cast<unsigned *>(A.q + A.s.scales + (rt / 4 * A.s.col_tiles + kt) * MX_SCALE_TILE_BYTES + b * 64 + sub * 4) = scales;
+        }
+    }
+    if constexpr (QT) {
+        __syncthreads();
+        const unsigned *words = reinterpret_cast<const unsigned *>(tile);
+        const int lane = tid & 63, wave = sl_uniform(tid >> 6);
+        const long long ct0 = kt * 8, kt2 = row0 / MX_COLS;            // row tiles of qt from here, its column tile
+        const int b = B16 ? wave : (int)(row0 / 32 & 3) + (wave >> 1);
+        // one column's codes and scale byte
+        auto put = [&](int c, sl_u4 w, unsigned x) __attribute__((always_inline)) {
+            const long long ct = ct0 + (c >> 4);
+            if (ct < A.t.row_tiles)
+                *reinterpret_cast<sl_u4 *>(A.qt + (ct * A.t.col_tiles + kt2) * MX_TILE_BYTES + b * 256 + (c & 15) * 16) = w;
+            if (ct < (A.t.row_tiles + 3) / 4 * 4)
+                A.qt[A.t.scales + (ct / 4 * A.t.col_tiles + kt2) * MX_SCALE_TILE_BYTES + b * 64 + (c & 15) * 4 + (ct & 3)] = (unsigned char)x;
+        };
+        if constexpr (B16) {
+            unsigned e[32], t = 0;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                e[i] = words[(wave * 32 + i) * 64 + lane];
+                t = sl_pair_max(t, e[i] & 0x7FFF7FFFu);
+            }
+            const unsigned x0 = sl_mx4_scale(t << 16), x1 = sl_mx4_scale(t & 0xFFFF0000u);
+            const float f0 = sl_mx4_factor(x0), f1 = sl_mx4_factor(x1);
+            sl_u4 w0, w1;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                unsigned o0 = 0, o1 = 0;
+#define SL_PAIR(J)                                                                       \
+    o0 = sl_mx4_pair<J>(o0, __builtin_amdgcn_perm(e[8 * i + 2 * J + 1], e[8 * i + 2 * J], 0x05040100u), f0); \
+    o1 = sl_mx4_pair<J>(o1, __builtin_amdgcn_perm(e[8 * i + 2 * J + 1], e[8 * i + 2 * J], 0x07060302u), f1);
+                SL_PAIR(0) SL_PAIR(1) SL_PAIR(2) SL_PAIR(3)
+#undef SL_PAIR
+                w0[i] = x0 == 255u ? 0u : o0, w1[i] = x1 == 255u ? 0u : o1;
+            }
+            put(lane * 2, w0, x0);
+            put(lane * 2 + 1, w1, x1);
+        } else {
+            const int c = (wave & 1) * 64 + lane;
+            SlOctet<false> e[4];
+            unsigned t = 0;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) e[i >> 3].w[i & 7] = words[((wave >> 1) * 32 + i) * 128 + c];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t = max(t, e[i].top());
+            const unsigned x = sl_mx4_scale(t);
+            put(c, sl_u4{e[0].pack(x), e[1].pack(x), e[2].pack(x), e[3].pack(x)}, x);
+        }
+    }
 }
 
-// A lane per block again.
+// Eight elements - a word of codes - in a lane, 16 lanes to a row of a tile.
 template <bool B16>
 __global__ void __launch_bounds__(256) k_dequantize(const unsigned char *q, SlMx4Shape s, void *out, long long ld)
 {
-    const float grid[8] = {0.0f, 0.5f, 1.0f, 1.5f, 2.0f, 3.0f, 4.0f, 6.0f};
-    const int lane = threadIdx.x & 63, wave = sl_uniform((int)(threadIdx.x >> 6));
-    const long long tile = (long long)blockIdx.x * 4 + wave;
-    if (tile >= s.row_tiles * s.col_tiles) return;
-    const long long rt = tile / s.col_tiles, kt = tile % s.col_tiles;
-    const long long row = rt * MX_ROWS + (lane & 15), col = kt * MX_COLS + (lane >> 4) * MX_BLOCK;
-    if (row >= s.rows) return;
-    const sl_u4 w = *reinterpret_cast<const sl_u4 *>(q + tile * MX_TILE_BYTES + lane * 16);
-    const float f = sl_mx4_factor(q[s.scales + ((rt >> 2) * s.col_tiles + kt) * MX_SCALE_TILE_BYTES + lane * 4 + (rt & 3)]);
+    typedef unsigned u4a __attribute__((ext_vector_type(4), aligned(2)));
+    const int octet = threadIdx.x & 15, sub = threadIdx.x >> 4, b = octet >> 2;
+    const long long rg = blockIdx.x / s.col_tiles, kt = blockIdx.x % s.col_tiles;
+    const long long col = kt * MX_COLS + octet * 8;
+    const int n = (int)max(min(s.cols - col, 8ll), 0ll);
+    const unsigned scales = *reinterpret_cast<const unsigned *>(q + s.scales + (rg * s.col_tiles + kt) * MX_SCALE_TILE_BYTES + b * 64 + sub * 4);
+    unsigned code[4];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        if (col + i >= s.cols) return;
-        const unsigned c = w[i >> 3] >> (4 * (i & 7)) & 15u;
-        float x = grid[c & 7u] * f;
-        if (c & 8u) x = -x;
-        const long long at = row * ld + col + i;
-        if constexpr (B16) static_cast<unsigned short *>(out)[at] = (unsigned short)sl_bf16_bits(x);
-        else static_cast<float *>(out)[at] = x;
+    for (int i = 0; i < 4; ++i) {
+        const long long rt = min(rg * 4 + i, s.row_tiles - 1);
+        code[i] = *reinterpret_cast<const unsigned *>(q + (rt * s.col_tiles + kt) * MX_TILE_BYTES + b * 256 + sub * 16 + (octet & 3) * 4);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const long long row = (rg * 4 + i) * 16 + sub;
+        if (row >= s.rows) return;
+        const unsigned x = scales >> (8 * i) & 255u;
+        const float f = sl_mx4_factor(x);
+        typedef float f2 __attribute__((ext_vector_type(2)));
+        const f2 p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[i], f, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[i], f, 1);
+        const f2 p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[i], f, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[i], f, 3);
+        float e[8] = {p0.x, p0.y, p1.x, p1.y, p2.x, p2.y, p3.x, p3.y};
+        if (x == 255u) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) e[j] = f;
+        }
+        const long long at = row * ld + col;
+        if constexpr (B16) {
+            unsigned short *o = static_cast<unsigned short *>(out) + at;
+            const sl_u4 w = {sl_bf16_pair(e[0], e[1]), sl_bf16_pair(e[2], e[3]), sl_bf16_pair(e[4], e[5]), sl_bf16_pair(e[6], e[7])};
+            if (n >= 8) {
+                *reinterpret_cast<u4a *>(o) = w;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 7; ++j)
+                    if (j < n) o[j] = (unsigned short)(w[j >> 1] >> (16 * (j & 1)));
+            }
+        } else {
+            float *o = static_cast<float *>(out) + at;
+            if (n >= 8) {
+                typedef float f4a __attribute__((ext_vector_type(4), aligned(4)));
+                *reinterpret_cast<f4a *>(o) = sl_f4{e[0], e[1], e[2], e[3]};
+                *reinterpret_cast<f4a *>(o + 4) = sl_f4{e[4], e[5], e[6], e[7]};
+            } else {
+#pragma unroll
+                for (int j = 0; j < 7; ++j)
+                    if (j < n) o[j] = e[j];
+            }
+        }
     }
 }
 
@@ -70,18 +176,12 @@ int check_launch()
 
 bool misaligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
 
-template <bool T>
-int quantize(const void *src, int type, long long rows, long long cols, long long ld, unsigned char *q, hipStream_t st)
+template <bool B16>
+void launch(const QuantArgs &A, unsigned groups, hipStream_t st)
 {
-    SlMx4Shape s;
-    if (!sl_mx4_shape(T ? cols : rows, T ? rows : cols, s)) return SL_ERR_INVALID_ARG;
-    QuantArgs A;
-    A.src = src, A.rows = rows, A.cols = cols, A.ld = ld, A.q = q;
-    A.row_tiles = s.row_tiles, A.col_tiles = s.col_tiles, A.scales = s.scales;
-    A.groups = (s.row_tiles + 3) / 4 * 4;
-    const dim3 grid((unsigned)((A.groups * A.col_tiles + 3) / 4));
-    hipLaunchKernelGGL((type == SL_TYPE_BF16 ? k_quantize<true, T> : k_quantize<false, T>), grid, dim3(256), 0, st, A);
-    return check_launch();
+    if (A.q && A.qt) hipLaunchKernelGGL((k_quantize<B16, true, true>), dim3(groups), dim3(256), 0, st, A);
+    else if (A.q) hipLaunchKernelGGL((k_quantize<B16, true, false>), dim3(groups), dim3(256), 0, st, A);
+    else hipLaunchKernelGGL((k_quantize<B16, false, true>), dim3(groups), dim3(256), 0, st, A);
 }
 
 }  // namespace
@@ -89,11 +189,16 @@ int quantize(const void *src, int type, long long rows, long long cols, long lon
 int slk_mx4_quantize(const void *src, int type, long long rows, long long cols, long long ld, unsigned char *q, unsigned char *qt,
                      hipStream_t st)
 {
-    if (q)
-        if (const int rc = quantize<false>(src, type, rows, cols, ld, q, st)) return rc;
-    if (qt)
-        if (const int rc = quantize<true>(src, type, rows, cols, ld, qt, st)) return rc;
-    return SL_OK;
+    QuantArgs A;
+    if (!sl_mx4_shape(rows, cols, A.s) || !sl_mx4_shape(cols, rows, A.t)) return SL_ERR_INVALID_ARG;
+    A.src = src, A.rows = rows, A.cols = cols, A.ld = ld, A.q = q, A.qt = qt;
+    A.col_groups = A.s.col_tiles;
+    // qt's tiles are 128 of these rows deep and are filled up, also past the last row
+    const long long row_groups = type == SL_TYPE_BF16 ? (rows + 127) / 128 : qt ? (rows + 127) / 128 * 2 : (rows + 63) / 64;
+    const unsigned groups = (unsigned)(row_groups * A.col_groups);
+    if (type == SL_TYPE_BF16) launch<true>(A, groups, st);
+    else launch<false>(A, groups, st);
+    return check_launch();
 }
 
 extern "C" {
@@ -106,8 +211,9 @@ size_t sl_mx4_bytes(int64_t rows, int64_t cols)
 
 int sl_mx4_quantize(const void *src, int src_type, int64_t rows, int64_t cols, int64_t ld, void *q, void *qt, void *stream)
 {
-    SlMx4Shape s;
-    if (!src || (!q && !qt) || q == qt || q == src || qt == src || !sl_mx4_shape(rows, cols, s)) return SL_ERR_INVALID_ARG;
+    SlMx4Shape s, t;
+    if (!src || (!q && !qt) || q == qt || q == src || qt == src || !sl_mx4_shape(rows, cols, s) || !sl_mx4_shape(cols, rows, t))
+        return SL_ERR_INVALID_ARG;
     if (src_type != SL_TYPE_F32 && src_type != SL_TYPE_BF16) return SL_ERR_INVALID_ARG;
     if (ld < cols || ld > ((int64_t)1 << 40) || misaligned(q, 16) || misaligned(qt, 16) || misaligned(src, src_type == SL_TYPE_BF16 ? 2 : 4))
         return SL_ERR_INVALID_ARG;
@@ -121,7 +227,7 @@ int sl_mx4_dequantize(const void *q, int64_t rows, int64_t cols, void *out, int 
     if (!q || !out || q == out || !sl_mx4_shape(rows, cols, s)) return SL_ERR_INVALID_ARG;
     if (out_type != SL_TYPE_F32 && out_type != SL_TYPE_BF16) return SL_ERR_INVALID_ARG;
     if (ld < cols || ld > ((int64_t)1 << 40) || misaligned(q, 16) || misaligned(out, out_type == SL_TYPE_BF16 ? 2 : 4)) return SL_ERR_INVALID_ARG;
-    const dim3 grid((unsigned)((s.row_tiles * s.col_tiles + 3) / 4));
+    const dim3 grid((unsigned)((s.row_tiles + 3) / 4 * s.col_tiles));
     hipLaunchKernelGGL(out_type == SL_TYPE_BF16 ? k_dequantize<true> : k_dequantize<false>, grid, dim3(256), 0,
                        static_cast<hipStream_t>(stream), static_cast<const unsigned char *>(q), s, out, (long long)ld);
     return check_launch();
