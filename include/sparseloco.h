@@ -427,11 +427,12 @@ int sl_adamw_state_values(sl_adamw *opt, int moment, const uint8_t *codes, const
  * of a row, the last block of a row possibly short.  X is the smallest with every element of the block
  * <= 6 * 2^(X-127) - none is cut off; elements are rounded to nearest, ties to the even code.  A block with
  * an infinity or a NaN has X = 255 and is NaN as a whole.
- * In memory: the codes in tiles of 16 rows x 128 columns, row tile by row tile - in a tile, block
- * b = 0..3 of row r is the 16 bytes at 256*b + 16*r, element 2i in the low half of byte i; then the scales
- * in tiles of 64 rows x 128 columns - the byte of block b of row r is at 64*b + 4*(r mod 16) + r/16.
+ * In memory: the codes in tiles of 32 rows x 128 columns, row tile by row tile - in a tile, block
+ * b = 0..3 of row r is the 16 bytes at 512*b + 16*r, element 2i in the low half of byte i; then the scales
+ * in tiles of 64 rows x 128 columns - the byte of block b of row r is at 128*(b mod 2) + 4*(r mod 32)
+ * + 2*(r/32) + b/2.
  * Rows and columns that fill up tiles are zero.  sl_mx4_bytes() is the size (0 for a size that is not
- * positive or has more than 2^25 tiles of codes); 16-byte aligned. */
+ * positive or has more than 2^24 tiles of codes); 16-byte aligned. */
 size_t sl_mx4_bytes(int64_t rows, int64_t cols);
 
 /* src     in,  device, rows x cols of src_type, row r at element r*ld (ld >= cols), aligned to its element

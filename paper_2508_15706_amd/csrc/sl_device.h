@@ -235,6 +235,8 @@ SL_DEV unsigned sl_work_group(unsigned i, unsigned order)
 #define SL_DPP_XOR2 0x4E
 #define SL_DPP_HALF_MIRROR 0x141
 #define SL_DPP_MIRROR 0x140
+//   SL_DPP_ROW_ROR8           lane i reads lane i ^ 8 (its row of 16 turned by 8).
+#define SL_DPP_ROW_ROR8 0x128
 // (every lane has a source lane, so there is no old value to keep: the move needs no copy of v first and
 // can become an operand of the instruction that uses it)
 template <int CTRL>

@@ -1,22 +1,26 @@
 // Layout of the microscaled 4-bit matrices (include/sparseloco.h) and the conversions to and from them.
 //
-// The layout is that of the matrix unit's operands: in the 16 x 16 x 128 product of 4-bit operands lane l holds block
-// l / 16 of row l % 16 - 16 bytes - and one byte of a register gives the block's scale.  A tile of 16 rows x 128
-// columns is therefore 1 KB that a wave loads in lane order, and the scale tile of 64 rows is one word per lane
-// whose four bytes serve four such tiles.
+// The layout is that of the matrix unit's operands: in the 32 x 32 x 64 product of 4-bit operands lane l holds block
+// l / 32 of row l % 32 - 16 bytes - and one byte of a register gives the block's scale.  A tile of 32 rows x 128
+// columns is therefore two operands of 1 KB that a wave loads in lane order, and the scale tile of 64 rows is one
+// word per lane whose four bytes serve the four operands of 64 rows x 128 columns.
 #pragma once
 #include "sl_device.h"
 
-enum { MX_ROWS = 16, MX_COLS = 128, MX_BLOCK = 32, MX_TILE_BYTES = 1024, MX_SCALE_ROWS = 64, MX_SCALE_TILE_BYTES = 256,
-       MX_MOST_TILES = 1 << 25 };      // (a grid has less than 2^32 threads)
+enum { MX_ROWS = 32, MX_COLS = 128, MX_BLOCK = 32, MX_TILE_BYTES = 2048, MX_SCALE_ROWS = 64, MX_SCALE_TILE_BYTES = 256,
+       MX_MOST_TILES = 1 << 24 };      // (a grid has less than 2^32 threads)
 
 struct SlMx4Shape {
     long long rows, cols;
-    long long row_tiles;        // tiles of 16 rows
+    long long row_tiles;        // tiles of 32 rows
     long long col_tiles;        // tiles of 128 columns
     long long scales;           // byte offset of the scales
     long long bytes;
 };
+
+// Offsets of block b of row r in its tile of codes and of its byte in its tile of scales.
+__host__ __device__ inline int sl_mx4_code_at(int r, int b) { return 512 * b + 16 * (r & 31); }
+__host__ __device__ inline int sl_mx4_scale_at(int r, int b) { return 128 * (b & 1) + 4 * (r & 31) + 2 * (r >> 5 & 1) + (b >> 1); }
 
 // False where sl_mx4_bytes is 0.
 inline bool sl_mx4_shape(long long rows, long long cols, SlMx4Shape &s)

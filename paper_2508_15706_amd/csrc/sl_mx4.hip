@@ -16,8 +16,8 @@ struct QuantArgs {
 // time, 16 rows per access.
 //
 // Along the rows (Q) a block is a quad of lanes: its largest magnitude comes by two lane moves, its codes are one word
-// a lane, and the 256 threads' words of an access are one tile of codes, 1 KB.  A block's scale byte and those of the
-// same block 16, 32 and 48 rows on are the word that the first lane of the quad writes.
+// a lane, and the 256 threads' words of two accesses are one tile of codes, 2 KB.  The scale bytes of blocks 0 and 2 (1 and
+// 3) of a row and of the row 32 on are the word that the first lane of the quad writes.
 // Along the columns (QT) the elements pass through LDS as they are; a lane then has 32 rows of two columns (bf16, one
 // wave for each block of 32 rows) or of one (fp32, two waves), read row by row without bank conflicts.
 template <bool B16, bool Q, bool QT>
@@ -46,33 +46,37 @@ __global__ void __launch_bounds__(256) k_quantize(QuantArgs A)
         const int b = octet >> 2;
 #pragma unroll
         for (int i = 0; i < ROWS / 16; i += 4) {
-            const long long rt = row0 / 16 + i;
-            unsigned scales = 0;
+            const long long rt = row0 / MX_ROWS + i / 2;               // row tile of access i; i + 2 begins the next
+            unsigned x[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const unsigned x = sl_mx4_scale(sl_quad_max(v[i + j].top()));
-                scales |= x << (8 * j);
-                const unsigned w = v[i + j].pack(x);
-                if (rt + j < A.s.row_tiles)
-                    *reinterpret_cast<unsigned *>(A.q + ((rt + j) * A.s.col_tiles + kt) * MX_TILE_BYTES + b * 256 + sub * 16 + (octet & 3) * 4) = w;
+                x[j] = sl_mx4_scale(sl_quad_max(v[i + j].top()));
+                const unsigned w = v[i + j].pack(x[j]);
+                if (rt + j / 2 < A.s.row_tiles)
+                    *reinterpret_cast<unsigned *>(A.q + ((rt + j / 2) * A.s.col_tiles + kt) * MX_TILE_BYTES +
+                                                  sl_mx4_code_at((j & 1) * 16 + sub, b) + (octet & 3) * 4) = w;
+                x[j] |= (unsigned)sl_dpp<SL_DPP_ROW_ROR8>((int)x[j]) << 8;       // lanes of blocks 0 and 1: those of 2 and 3
             }
-            if ((octet & 3) == 0 && rt < A.s.row_tiles)
-                *reinterpret_cast<unsigned *>(A.q + A.s.scales + (rt / 4 * A.s.col_tiles + kt) * MX_SCALE_TILE_BYTES + b * 64 + sub * 4) = scales;
+            if ((octet & 3) == 0 && octet < 8 && rt < A.s.row_tiles) {
+                unsigned *to = reinterpret_cast<unsigned *>(A.q + A.s.scales + (rt / 2 * A.s.col_tiles + kt) * MX_SCALE_TILE_BYTES);
+                to[sl_mx4_scale_at(sub, b) / 4] = x[0] | x[2] << 16;
+                to[sl_mx4_scale_at(16 + sub, b) / 4] = x[1] | x[3] << 16;
+            }
         }
     }
     if constexpr (QT) {
         __syncthreads();
         const unsigned *words = reinterpret_cast<const unsigned *>(tile);
         const int lane = tid & 63, wave = sl_uniform(tid >> 6);
-        const long long ct0 = kt * 8, kt2 = row0 / MX_COLS;            // row tiles of qt from here, its column tile
+        const long long ct0 = kt * 4, kt2 = row0 / MX_COLS;            // row tiles of qt from here, its column tile
         const int b = B16 ? wave : (int)(row0 / 32 & 3) + (wave >> 1);
         // one column's codes and scale byte
         auto put = [&](int c, sl_u4 w, unsigned x) __attribute__((always_inline)) {
-            const long long ct = ct0 + (c >> 4);
+            const long long ct = ct0 + (c >> 5);
             if (ct < A.t.row_tiles)
-                *reinterpret_cast<sl_u4 *>(A.qt + (ct * A.t.col_tiles + kt2) * MX_TILE_BYTES + b * 256 + (c & 15) * 16) = w;
-            if (ct < (A.t.row_tiles + 3) / 4 * 4)
-                A.qt[A.t.scales + (ct / 4 * A.t.col_tiles + kt2) * MX_SCALE_TILE_BYTES + b * 64 + (c & 15) * 4 + (ct & 3)] = (unsigned char)x;
+                *reinterpret_cast<sl_u4 *>(A.qt + (ct * A.t.col_tiles + kt2) * MX_TILE_BYTES + sl_mx4_code_at(c, b)) = w;
+            if (ct < (A.t.row_tiles + 1) / 2 * 2)
+                A.qt[A.t.scales + (ct / 2 * A.t.col_tiles + kt2) * MX_SCALE_TILE_BYTES + sl_mx4_scale_at(c, b)] = (unsigned char)x;
         };
         if constexpr (B16) {
             unsigned e[32], t = 0;
@@ -119,18 +123,19 @@ __global__ void __launch_bounds__(256) k_dequantize(const unsigned char *q, SlMx
     const long long rg = blockIdx.x / s.col_tiles, kt = blockIdx.x % s.col_tiles;
     const long long col = kt * MX_COLS + octet * 8;
     const int n = (int)max(min(s.cols - col, 8ll), 0ll);
-    const unsigned scales = *reinterpret_cast<const unsigned *>(q + s.scales + (rg * s.col_tiles + kt) * MX_SCALE_TILE_BYTES + b * 64 + sub * 4);
-    unsigned code[4];
+    const unsigned char *scales = q + s.scales + (rg * s.col_tiles + kt) * MX_SCALE_TILE_BYTES;
+    unsigned code[4], byte[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const long long rt = min(rg * 4 + i, s.row_tiles - 1);
-        code[i] = *reinterpret_cast<const unsigned *>(q + (rt * s.col_tiles + kt) * MX_TILE_BYTES + b * 256 + sub * 16 + (octet & 3) * 4);
+        const long long rt = min(rg * 2 + i / 2, s.row_tiles - 1);
+        code[i] = *reinterpret_cast<const unsigned *>(q + (rt * s.col_tiles + kt) * MX_TILE_BYTES + sl_mx4_code_at((i & 1) * 16 + sub, b) + (octet & 3) * 4);
+        byte[i] = scales[sl_mx4_scale_at(i * 16 + sub, b)];
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const long long row = (rg * 4 + i) * 16 + sub;
+        const long long row = rg * 64 + i * 16 + sub;
         if (row >= s.rows) return;
-        const unsigned x = scales >> (8 * i) & 255u;
+        const unsigned x = byte[i];
         const float f = sl_mx4_factor(x);
         typedef float f2 __attribute__((ext_vector_type(2)));
         const f2 p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[i], f, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[i], f, 1);
@@ -227,7 +232,7 @@ int sl_mx4_dequantize(const void *q, int64_t rows, int64_t cols, void *out, int 
     if (!q || !out || q == out || !sl_mx4_shape(rows, cols, s)) return SL_ERR_INVALID_ARG;
     if (out_type != SL_TYPE_F32 && out_type != SL_TYPE_BF16) return SL_ERR_INVALID_ARG;
     if (ld < cols || ld > ((int64_t)1 << 40) || misaligned(q, 16) || misaligned(out, out_type == SL_TYPE_BF16 ? 2 : 4)) return SL_ERR_INVALID_ARG;
-    const dim3 grid((unsigned)((s.row_tiles + 3) / 4 * s.col_tiles));
+    const dim3 grid((unsigned)((s.row_tiles + 1) / 2 * s.col_tiles));
     hipLaunchKernelGGL(out_type == SL_TYPE_BF16 ? k_dequantize<true> : k_dequantize<false>, grid, dim3(256), 0,
                        static_cast<hipStream_t>(stream), static_cast<const unsigned char *>(q), s, out, (long long)ld);
     return check_launch();

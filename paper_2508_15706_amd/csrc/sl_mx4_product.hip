@@ -13,7 +13,7 @@ typedef int v8i __attribute__((ext_vector_type(8)));
 
 struct ProductArgs {
     const unsigned char *a, *b;
-    long long a_tiles, b_tiles;          // row tiles of 16
+    long long a_tiles, b_tiles;          // row tiles of 32
     long long k_tiles;                   // column tiles of 128
     long long a_scales, b_scales;        // byte offsets
     long long m, n;
@@ -23,12 +23,17 @@ struct ProductArgs {
     int accumulate;
 };
 
-// One step of 128 of the contraction for a tile of 16 x 16: row i of the result is b's row i, column j a's row j.
+typedef float sl_f16 __attribute__((ext_vector_type(16)));
+
+// One step of 64 of the contraction for a tile of 32 x 32: row i of the result is b's row i, column j a's row j; lane l
+// has column l % 32 and of it the rows 8 g + 4 (l / 32) + e, g, e = 0 .. 3, at 4 g + e.
+// (Of the two shapes of the instruction this one is fed with half the instructions: nothing but products on random
+// operands in registers, one / two / four waves per SIMD, PFLOP/s: 32 x 32 x 64 5.9 / 6.6 / 6.7, 16 x 16 x 128 4.3 / 5.2 / 6.1.)
 template <int OB, int OA>
-SL_DEV sl_f4 mx4_step(sl_u4 b, sl_u4 a, sl_f4 c, unsigned sb, unsigned sa)
+SL_DEV sl_f16 mx4_step(sl_u4 b, sl_u4 a, sl_f16 c, unsigned sb, unsigned sa)
 {
     const v8i x = {(int)b.x, (int)b.y, (int)b.z, (int)b.w, 0, 0, 0, 0}, y = {(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, OB, (int)sb, OA, (int)sa);
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, OB, (int)sb, OA, (int)sa);
 }
 
 // Eight consecutive columns of a row of c.
@@ -95,16 +100,17 @@ SL_DEV void stage_barrier()
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
-// Four waves, 2 x 2, TM x TN tiles of 16 x 16 each: 32 TM x 32 TN of c in a workgroup.  Per step of 128 of the
-// contraction a stage of LDS holds the workgroup's operands as they lie in memory - a tile is what a wave reads in lane order -
-// and four stages are filled ahead; a wave's operands of the next step are read into registers while the matrix unit works on this one's.
-// Row i of the result's tile j is not b's row 16 j + i: of each 32 rows of b, a pair of tiles takes 8 (i / 4) + i % 4 and those 4 on,
-// so that a lane has eight consecutive columns of c and writes 16 bytes of bf16 (32 of fp32).
+// Four waves, 2 x 2, TM x TN tiles of 32 x 32 each: 64 TM x 64 TN of c in a workgroup.  Per step of 128 of the
+// contraction a stage of LDS holds the workgroup's operands as they lie in memory - an operand is what a wave reads in lane
+// order - and four stages are filled ahead; a wave's operands of the next step are read into registers while the matrix unit works
+// on this one's.
+// Row i of a result's tile is not b's row i: i = 8 g + 4 q + e takes 16 (g / 2) + 8 q + 4 (g % 2) + e, so that a lane has
+// eight consecutive columns of c twice and writes them 16 bytes (bf16) at a time.
 template <bool B16, int TM, int TN>
-__global__ void __launch_bounds__(256, TM * TN > 32 ? 1 : 2) k_product(ProductArgs A)
+__global__ void __launch_bounds__(256, 2) k_product(ProductArgs A)
 {
     constexpr int CODES = (2 * TM + 2 * TN) * MX_TILE_BYTES, STAGE = CODES + 2048, STAGES = 4;
-    constexpr int PER_WAVE = (TM + TN) / 2, D = PER_WAVE + 1;       // loads of a wave per stage
+    constexpr int PER_WAVE = TM + TN, D = PER_WAVE + 1;             // loads of a wave per stage, 1 KB each
     extern __shared__ __align__(16) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = sl_uniform((int)(threadIdx.x >> 6)), wm = wave >> 1, wn = wave & 1;
     const TilePlace at = tile_place(blockIdx.x, gridDim.x, A.m_tiles, A.n_tiles);
@@ -115,88 +121,84 @@ __global__ void __launch_bounds__(256, TM * TN > 32 ? 1 : 2) k_product(ProductAr
     const unsigned char *src[PER_WAVE];
 #pragma unroll
     for (int i = 0; i < PER_WAVE; ++i) {
-        const int t = wave + 4 * i;
-        src[i] = t < 2 * TM ? A.a + min(i0 + t, A.a_tiles - 1) * A.k_tiles * MX_TILE_BYTES
-                            : A.b + min(j0 + t - 2 * TM, A.b_tiles - 1) * A.k_tiles * MX_TILE_BYTES;
+        const int half = wave + 4 * i, t = half >> 1;
+        src[i] = (t < 2 * TM ? A.a + min(i0 + t, A.a_tiles - 1) * A.k_tiles * MX_TILE_BYTES
+                             : A.b + min(j0 + t - 2 * TM, A.b_tiles - 1) * A.k_tiles * MX_TILE_BYTES) + (half & 1) * 1024;
     }
     // even waves bring a's scales, odd ones b's: up to four tiles of 64 rows, 16 lanes each
     const unsigned char *scales = wave & 1 ? A.b + A.b_scales : A.a + A.a_scales;
-    const long long group0 = (wave & 1 ? j0 : i0) >> 2, groups = ((wave & 1 ? A.b_tiles : A.a_tiles) + 3) >> 2;
+    const long long group0 = (wave & 1 ? j0 : i0) >> 1, groups = ((wave & 1 ? A.b_tiles : A.a_tiles) + 1) >> 1;
     scales += min(group0, groups - 1) * A.k_tiles * MX_SCALE_TILE_BYTES;
     const unsigned scale_off = (unsigned)((min(group0 + (lane >> 4), groups - 1) - min(group0, groups - 1)) * A.k_tiles * MX_SCALE_TILE_BYTES) + (lane & 15) * 16;
 
     // (past the last step it brings that one again, so that every step waits for the same number of loads)
     auto fill = [&](int at) __attribute__((always_inline)) {
         const unsigned to = lds0 + (unsigned)(at & (STAGES - 1)) * STAGE;
-        const int s = min(at, steps - 1);
+        const long long s = min(at, steps - 1);
 #pragma unroll
-        for (int i = 0; i < PER_WAVE; ++i) dma16(src[i] + (long long)s * MX_TILE_BYTES, lane * 16, to + (wave + 4 * i) * MX_TILE_BYTES);
-        dma16(scales + (long long)s * MX_SCALE_TILE_BYTES, scale_off, to + CODES + (wave & 1) * 1024);
+        for (int i = 0; i < PER_WAVE; ++i) dma16(src[i] + s * MX_TILE_BYTES, lane * 16, to + (wave + 4 * i) * 1024);
+        dma16(scales + s * MX_SCALE_TILE_BYTES, scale_off, to + CODES + (wave & 1) * 1024);
     };
 
-    // where in b's 32 rows this lane's row of a tile lies, even and odd tiles
-    const int r0 = 8 * ((lane & 15) >> 2) + (lane & 3);
-    const int b_off = (r0 >> 4) * MX_TILE_BYTES + (lane >> 4) * 256 + (r0 & 15) * 16;
-    const int b_scale = (lane >> 4) * 64 + (r0 & 15) * 4, b_shift = 8 * (r0 >> 4);
+    // b's row that this lane has in a tile
+    const int i = lane & 31, r = 16 * (i >> 4) + 8 * (i >> 2 & 1) + 4 * (i >> 3 & 1) + (i & 3);
+    const int b_off = (lane >> 5) * 512 + r * 16, b_scale = (lane >> 5) * 128 + r * 4;
 
-    sl_u4 a[2][TM], b[2][TN];
-    unsigned sa[2][TM / 4], sb[2][TN / 2];
+    sl_u4 a[2][TM][2], b[2][TN][2];
+    unsigned sa[2][TM / 2], sb[2][TN / 2];
+    constexpr int READS = TM / 2 + TN / 2 + 2 * (TM + TN);
     auto read = [&](int s, auto set) __attribute__((always_inline)) {
         constexpr int S = decltype(set)::value;
         const unsigned char *st = lds + (s & (STAGES - 1)) * STAGE;
 #pragma unroll
-        for (int t = 0; t < TM / 4; ++t) sa[S][t] = *reinterpret_cast<const unsigned *>(st + CODES + (wm * (TM / 4) + t) * 256 + lane * 4);
+        for (int t = 0; t < TM / 2; ++t) sa[S][t] = *reinterpret_cast<const unsigned *>(st + CODES + (wm * (TM / 2) + t) * 256 + lane * 4);
 #pragma unroll
-        for (int t = 0; t < TN / 2; ++t)
-            sb[S][t] = *reinterpret_cast<const unsigned *>(st + CODES + 1024 + (wn * (TN / 4) + t / 2) * 256 + b_scale + (t & 1) * 16);
+        for (int t = 0; t < TN / 2; ++t) sb[S][t] = *reinterpret_cast<const unsigned *>(st + CODES + 1024 + (wn * (TN / 2) + t) * 256 + b_scale);
 #pragma unroll
-        for (int t = 0; t < TN; ++t)
-            b[S][t] = *reinterpret_cast<const sl_u4 *>(st + (2 * TM + wn * TN + (t & ~1)) * MX_TILE_BYTES + b_off + (t & 1) * 64);
+        for (int h = 0; h < 2; ++h) {
 #pragma unroll
-        for (int t = 0; t < TM; ++t) a[S][t] = *reinterpret_cast<const sl_u4 *>(st + (wm * TM + t) * MX_TILE_BYTES + lane * 16);
+            for (int t = 0; t < TN; ++t) b[S][t][h] = *reinterpret_cast<const sl_u4 *>(st + (2 * TM + wn * TN + t) * MX_TILE_BYTES + h * 1024 + b_off);
+#pragma unroll
+            for (int t = 0; t < TM; ++t) a[S][t][h] = *reinterpret_cast<const sl_u4 *>(st + (wm * TM + t) * MX_TILE_BYTES + h * 1024 + lane * 16);
+        }
     };
-    sl_f4 acc[TM][TN];
+    sl_f16 acc[TM][TN];
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = sl_f4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
     auto multiply = [&](auto set) __attribute__((always_inline)) {
         constexpr int S = decltype(set)::value;
-        unsigned sbs[TN / 2];
-#pragma unroll
-        for (int t = 0; t < TN / 2; ++t) sbs[t] = sb[S][t] >> b_shift;
-        // (the byte of a scale word that a tile takes is part of the instruction)
-        auto row = [&](auto ic) __attribute__((always_inline)) {
-            constexpr int I = decltype(ic)::value;
-#define MX4_AT(J) \
-    if constexpr (J < TN) acc[I][J] = mx4_step<(J & 2), I & 3>(b[S][J], a[S][I], acc[I][J], sbs[(J >> 2) * 2 + (J & 1)], sa[S][I >> 2]);
-            MX4_AT(0) MX4_AT(1) MX4_AT(2) MX4_AT(3) MX4_AT(4) MX4_AT(5) MX4_AT(6) MX4_AT(7)
-#undef MX4_AT
-        };
-#define MX4_ROW(I) if constexpr (I < TM) row(std::integral_constant<int, I>{});
-        MX4_ROW(0) MX4_ROW(1) MX4_ROW(2) MX4_ROW(3) MX4_ROW(4) MX4_ROW(5) MX4_ROW(6) MX4_ROW(7)
+        // (the byte of a scale word that an operand takes is part of the instruction)
+#define MX4_AT(H, I, J) \
+    if constexpr (I < TM && J < TN) \
+        acc[I][J] = mx4_step<2 * (J & 1) + H, 2 * (I & 1) + H>(b[S][J][H], a[S][I][H], acc[I][J], sb[S][J >> 1], sa[S][I >> 1]);
+#define MX4_ROW(H, I) MX4_AT(H, I, 0) MX4_AT(H, I, 1) MX4_AT(H, I, 2) MX4_AT(H, I, 3)
+#define MX4_HALF(H) MX4_ROW(H, 0) MX4_ROW(H, 1) MX4_ROW(H, 2) MX4_ROW(H, 3)
+        MX4_HALF(0) MX4_HALF(1)
+#undef MX4_HALF
 #undef MX4_ROW
+#undef MX4_AT
     };
     // The next step's operands into registers, this one's into the matrix unit.  Between the two barriers of the scheduler
     // reads of LDS and products alternate; without them the compiler moves the products behind the next step's reads.
-    auto body = [&](int s, auto set) __attribute__((always_inline)) {
-        constexpr int S = decltype(set)::value;
-        read(s + 1, std::integral_constant<int, 1 - S>{});
-        multiply(set);
-        constexpr int READS = TM / 4 + TN / 2 + TM + TN, EACH = TM * TN / READS;
-#pragma unroll
-        for (int i = 0; i < READS; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);      // LDS
-            __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);   // products
-        }
-        __builtin_amdgcn_sched_barrier(0);
-    };
     auto step = [&](int s, auto set) __attribute__((always_inline)) {
+        constexpr int S = decltype(set)::value;
         wait_dma<2 * D>();
         stage_barrier();
         fill(s + 4);
         __builtin_amdgcn_sched_barrier(0);
-        body(s, set);
+        read(s + 1, std::integral_constant<int, 1 - S>{});
+        multiply(set);
+        constexpr int PRODUCTS = 2 * TM * TN, EACH = (READS + PRODUCTS - 1) / PRODUCTS;
+#pragma unroll
+        for (int i = 0; i < PRODUCTS; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);   // reads of LDS
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);      // products
+        }
+        __builtin_amdgcn_sched_barrier(0);
     };
     if (steps > 0) {
 #pragma unroll
@@ -216,13 +218,17 @@ __global__ void __launch_bounds__(256, TM * TN > 32 ? 1 : 2) k_product(ProductAr
     }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-        const long long row = (i0 + wm * TM + i) * 16 + (lane & 15);
+        const long long row = (i0 + wm * TM + i) * MX_ROWS + (lane & 31);
         if (row >= A.m) continue;
 #pragma unroll
-        for (int j = 0; j < TN; j += 2) {
-            const long long col = (j0 + wn * TN + j) * 16 + (lane >> 4) * 8;
-            store_octet<B16>(A, row, col, acc[i][j], acc[i][j + 1]);
-        }
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                const sl_f16 v = acc[i][j];
+                store_octet<B16>(A, row, (j0 + wn * TN + j) * MX_ROWS + 16 * p + (lane >> 5) * 8,
+                                 sl_f4{v[8 * p], v[8 * p + 1], v[8 * p + 2], v[8 * p + 3]},
+                                 sl_f4{v[8 * p + 4], v[8 * p + 5], v[8 * p + 6], v[8 * p + 7]});
+            }
     }
 }
 
@@ -250,8 +256,8 @@ bool bad_sizes(int64_t m, int64_t n, int64_t k)
 template <bool B16, int TM, int TN>
 void launch_tiles(ProductArgs A, hipStream_t st)
 {
-    A.m_tiles = (A.m + 32 * TM - 1) / (32 * TM);
-    A.n_tiles = (A.n + 32 * TN - 1) / (32 * TN);
+    A.m_tiles = (A.m + 64 * TM - 1) / (64 * TM);
+    A.n_tiles = (A.n + 64 * TN - 1) / (64 * TN);
     constexpr unsigned bytes = 4 * ((2 * TM + 2 * TN) * MX_TILE_BYTES + 2048);
     static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_product<B16, TM, TN>),
                                                           hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
@@ -272,8 +278,8 @@ int product(const unsigned char *a, const unsigned char *b, int64_t m, int64_t n
     A.a_tiles = sa.row_tiles, A.b_tiles = sb.row_tiles, A.k_tiles = k > 0 ? sa.col_tiles : 0;
     A.a_scales = sa.scales, A.b_scales = sb.scales;
     A.m = m, A.n = n, A.c = c, A.ldc = ldc, A.accumulate = accumulate;
-    if (type == SL_TYPE_BF16) launch_tiles<true, 4, 4>(A, st);
-    else launch_tiles<false, 4, 4>(A, st);
+    if (type == SL_TYPE_BF16) launch_tiles<true, 2, 2>(A, st);
+    else launch_tiles<false, 2, 2>(A, st);
     return check_launch();
 }
 

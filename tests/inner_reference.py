@@ -36,13 +36,14 @@ def mx4_reference(x):
 def mx4_layout(buf, rows, cols):
     """(codes, scale bytes) of a 4-bit matrix as the header lays it out, tiles' padding included."""
     buf = np.asarray(buf, np.uint8)
-    rt, kt = -(-rows // 16), -(-cols // 128)
-    tiles = buf[:rt * kt * 1024].reshape(rt, kt, 4, 16, 16)               # row tile, column tile, block, row, byte
-    nib = np.stack([tiles & 15, tiles >> 4], -1).reshape(rt, kt, 4, 16, 32)
-    codes = nib.transpose(0, 3, 1, 2, 4).reshape(rt * 16, kt * 128)
+    rt, kt = -(-rows // 32), -(-cols // 128)
+    tiles = buf[:rt * kt * 2048].reshape(rt, kt, 4, 32, 16)               # row tile, column tile, block, row, byte
+    nib = np.stack([tiles & 15, tiles >> 4], -1).reshape(rt, kt, 4, 32, 32)
+    codes = nib.transpose(0, 3, 1, 2, 4).reshape(rt * 32, kt * 128)
     st = -(-rows // 64)
-    sc = buf[rt * kt * 1024:rt * kt * 1024 + st * kt * 256].reshape(st, kt, 4, 16, 4)   # scale tile, column tile, block, row % 16, row / 16
-    scales = sc.transpose(0, 4, 3, 1, 2).reshape(st * 64, kt * 4)
+    # scale tile, column tile, block % 2, row % 32, row / 32, block / 2
+    sc = buf[rt * kt * 2048:rt * kt * 2048 + st * kt * 256].reshape(st, kt, 2, 32, 2, 2)
+    scales = sc.transpose(0, 4, 3, 1, 5, 2).reshape(st * 64, kt * 4)
     return codes.astype(np.int64), scales.astype(np.int64)
 
 
