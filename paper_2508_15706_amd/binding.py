@@ -8,6 +8,7 @@ CPU fallback: if the library has not been built, importing symbols raises.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Optional, Sequence
 
@@ -604,6 +605,7 @@ def sl_adamw_state_values(opt: AdamW, moment: int, codes: torch.Tensor, scales: 
         raise SparseLoCoError("sl_adamw_state_values", st)
 
 
+@functools.lru_cache(maxsize=4096)                # (of the sizes alone; a call through ctypes costs as much as the rest of a binding)
 def sl_mx4_bytes(rows: int, cols: int) -> int:
     return int(lib().sl_mx4_bytes(int(rows), int(cols)))
 
@@ -612,6 +614,7 @@ def alloc_mx4(rows: int, cols: int, device="cuda") -> torch.Tensor:
     return torch.empty(max(16, sl_mx4_bytes(rows, cols)), dtype=torch.uint8, device=device)
 
 
+@functools.lru_cache(maxsize=4096)
 def sl_mx4_workspace_bytes(m: int, n: int, k: int) -> int:
     return int(lib().sl_mx4_workspace_bytes(int(m), int(n), int(k)))
 
