@@ -509,10 +509,14 @@ def _type_of(t: torch.Tensor) -> int:
 
 def _matrix(t: torch.Tensor):
     """(pointer, type, rows, cols, row stride) of a device matrix whose rows are contiguous."""
-    if not t.is_cuda or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError("expected a device matrix with contiguous rows")
-    rows, cols = t.shape
-    return t.data_ptr(), _type_of(t), rows, cols, (t.stride(0) if rows > 1 else max(cols, t.stride(0)))
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError("expected a device matrix")
+    (rows, cols), (ld, step), typ = t.shape, t.stride(), _TYPES.get(t.dtype)
+    if typ is None:
+        raise ValueError(f"expected float32 or bfloat16, got {t.dtype}")
+    if step != 1 and cols > 1:
+        raise ValueError("expected contiguous rows")
+    return t.data_ptr(), typ, rows, cols, (ld if rows > 1 else max(cols, ld))
 
 
 def _mx4_ptr(q: Optional[torch.Tensor], rows: int, cols: int) -> Optional[int]:
