@@ -3,6 +3,7 @@
 // of one tensor and belongs to one workgroup of four waves, wave w of which takes elements 1024 i + 256 w .. + 255 in
 // access i - one block of the 8-bit states, whose largest value is then a maximum over the wave's registers.
 #include <cmath>
+#include <type_traits>
 #include <cstring>
 #include <new>
 #include <vector>
@@ -14,7 +15,7 @@
 
 namespace {
 
-enum { UNIT = 4096, BLOCK = 256, NORM_GROUPS = 2048, MAX_UNITS = (1 << 24) - 1 };   // (a grid has less than 2^32 threads)
+enum { UNIT = 4096, BLOCK = 256, NORM_GROUPS = 2048, NORM_UNITS = 4, MAX_UNITS = (1 << 24) - 1 };   // (a grid has less than 2^32 threads)
 
 struct Unit {               // one 32-byte scalar load
     long long base;         // first element in the arenas
@@ -85,7 +86,11 @@ struct StepArgs {
     float b1, c1, b2, c2;            // beta1, 1 - beta1, beta2, 1 - beta2
     float rate, r, eps, shrink;      // lr/(1 - beta1^t), 1/sqrt(1 - beta2^t), eps, lr * weight_decay
     unsigned seed_hash;
+    unsigned order;                  // sl_work_group
 };
+
+// LDS that a workgroup of a long list asks for and does not use: two fit a compute unit then (see sl_outer.hip).
+enum { STREAM_LDS = 54272, STREAM8_LDS = 40960, SHORT_UNITS = 4096 };
 
 // One element: moments and parameter brought up to date.
 SL_DEV void adamw_update(const StepArgs &A, float keep, float scale, float grad, float &theta, float &m, float &v)
@@ -97,30 +102,52 @@ SL_DEV void adamw_update(const StepArgs &A, float keep, float scale, float grad,
     theta = theta * keep - __fdiv_rn(m * A.rate, den);
 }
 
-template <bool B16>
+// Long lists take one access of a unit after the other, with two workgroups to a compute unit (STREAM_LDS) and the
+// units in the order of sl_work_group: with more under way the memory has more rows open than it keeps.  Short ones, which give
+// a compute unit a few workgroups only, request a whole unit at once (SHORT).  us, so / SHORT: 1M elements 6.4 / 6.2, 4M
+// 23.6 / 20.0, 16M 80.9 / 80.3, 64M 315 / 322, 1.8B 8700 / 9260 (5.8 and 5.5 TB/s; 9250 without the order, 9180 with four
+// workgroups); two or four accesses at once on the 1.8B list 9070 and 9180.
+template <bool B16, bool SHORT>
 __global__ void __launch_bounds__(256) k_adamw(StepArgs A)
 {
-    const Unit u = A.units[blockIdx.x];
+    const Unit u = A.units[SHORT ? blockIdx.x : sl_work_group(blockIdx.x, A.order)];
     const float scale = A.grad_scale ? *A.grad_scale : 1.0f;
     if (scale != scale) return;
     const float keep = 1.0f - u.decay * A.shrink;
+    constexpr int STEP = SHORT ? 4 : 1;
+    auto part = [&](int q, auto is_full) __attribute__((always_inline)) {
+        constexpr bool full = decltype(is_full)::value;
+        auto place = [&](int i) -> long long { return u.base + ((q * STEP + i) * 1024 + (int)threadIdx.x * 4); };
+        auto exist = [&](int i) -> int { return full ? 4 : u.count - ((q * STEP + i) * 1024 + (int)threadIdx.x * 4); };
+        sl_f4 g[STEP], th[STEP], m[STEP], v[STEP];
 #pragma unroll
-    for (int i = 0; i < UNIT / 1024; ++i) {
-        const int at = i * 1024 + (int)threadIdx.x * 4, n = u.count - at;
-        if (n <= 0) return;
-        const long long p = u.base + at;
-        const sl_f4 g = load_grad<B16>(A.grad, p, n);
-        sl_f4 th = sl_load_edge(A.theta + p, n), m = sl_load_edge(A.m + p, n), v = sl_load_edge(A.v + p, n);
+        for (int i = 0; i < STEP; ++i) g[i] = load_grad<B16>(A.grad, place(i), exist(i));
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            float t = th[c], mm = m[c], vv = v[c];
-            adamw_update(A, keep, scale, g[c], t, mm, vv);
-            th[c] = t, m[c] = mm, v[c] = vv;
+        for (int i = 0; i < STEP; ++i) th[i] = sl_load_edge(A.theta + place(i), exist(i));
+#pragma unroll
+        for (int i = 0; i < STEP; ++i) m[i] = sl_load_edge(A.m + place(i), exist(i));
+#pragma unroll
+        for (int i = 0; i < STEP; ++i) v[i] = sl_load_edge(A.v + place(i), exist(i));
+#pragma unroll
+        for (int i = 0; i < STEP; ++i) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                float t = th[i][c], mm = m[i][c], vv = v[i][c];
+                adamw_update(A, keep, scale, g[i][c], t, mm, vv);
+                th[i][c] = t, m[i][c] = mm, v[i][c] = vv;
+            }
+            sl_store_edge(A.theta + place(i), exist(i), th[i]);
+            sl_store_edge(A.m + place(i), exist(i), m[i]);
+            sl_store_edge(A.v + place(i), exist(i), v[i]);
+            if (A.theta16) store_bf16(A.theta16 + place(i), exist(i), th[i]);
         }
-        sl_store_edge(A.theta + p, n, th);
-        sl_store_edge(A.m + p, n, m);
-        sl_store_edge(A.v + p, n, v);
-        if (A.theta16) store_bf16(A.theta16 + p, n, th);
+    };
+    if (u.count == UNIT) {
+#pragma unroll 1
+        for (int q = 0; q < UNIT / 1024 / STEP; ++q) part(q, std::true_type{});
+    } else {
+#pragma unroll 1
+        for (int q = 0; q < UNIT / 1024 / STEP; ++q) part(q, std::false_type{});
     }
 }
 
@@ -185,56 +212,74 @@ SL_DEV unsigned encode_v(float x, float inv, unsigned rnd)
     return max(min((b + rnd) >> 20, 255u), x > 0.0f ? 1u : 0u);
 }
 
-template <bool B16>
+// A wave has a block per access; a unit's four accesses are requested together.  Long lists: four workgroups to a compute
+// unit (STREAM8_LDS) in the order of sl_work_group, as in k_adamw.  us, so / as many workgroups as the registers allow, in list order: 64M
+// elements 176 / 174, 256M 740 / 802, 1.8B 5008 / 5396 (5.8 and 5.4 TB/s); two accesses at a time 5084, with two workgroups 7174; a lane with eight
+// elements in place of four writes its theta in pieces of 16 bytes that the streaming hint sends to memory by themselves: 6672 at best.
+template <bool B16, bool SHORT>
 __global__ void __launch_bounds__(256) k_adamw8(StepArgs A)
 {
-    const Unit u = A.units[blockIdx.x];
+    const Unit u = A.units[SHORT ? blockIdx.x : sl_work_group(blockIdx.x, A.order)];
     const float scale = A.grad_scale ? *A.grad_scale : 1.0f;
     if (scale != scale) return;
     const float keep = 1.0f - u.decay * A.shrink;
     const int lane = threadIdx.x & 63, wave = sl_uniform((int)(threadIdx.x >> 6));
+    constexpr int STEP = UNIT / 1024;
+    auto all = [&](auto is_full) __attribute__((always_inline)) {
+        constexpr bool full = decltype(is_full)::value;
+        sl_f4 g[STEP], th[STEP];
+        unsigned cm[STEP], cv[STEP];
+        float sm[STEP], sv[STEP];
+        // access i: a block of the wave; one that does not exist is read as the unit's first, and not written
+        auto first = [&](int i) -> int { return i * 1024 + wave * BLOCK; };
+        auto exist = [&](int i) -> int { return full ? 4 : u.count - first(i) - lane * 4; };
+        auto has = [&](int i) -> bool { return full || first(i) < u.count; };
+        auto place = [&](int i) -> long long { return u.base + (first(i) + lane * 4); };
+        auto block = [&](int i) -> int { return u.block0 + (has(i) ? first(i) / BLOCK : 0); };
 #pragma unroll
-    for (int i = 0; i < UNIT / 1024; ++i) {
-        const int first = i * 1024 + wave * BLOCK;
-        if (first >= u.count) return;                     // (the whole wave)
-        const int at = first + lane * 4, n = u.count - at;
-        const long long p = u.base + at;
-        const int block = u.block0 + first / BLOCK;
-        const sl_f4 g = load_grad<B16>(A.grad, p, n);
-        sl_f4 th = sl_load_edge(A.theta + p, n);
-        const unsigned cm = load_codes(A.m8 + p, n), cv = load_codes(A.v8 + p, n);
-        const float sm = block_scale(A.ms[block]), sv = block_scale(A.vs[block]);
-        float m[4], v[4];
-        int top_m = 0, top_v = 0;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            m[c] = decode_m(cm >> (8 * c) & 255u, sm);
-            v[c] = decode_v(cv >> (8 * c) & 255u, sv);
-            float t = th[c];
-            adamw_update(A, keep, scale, g[c], t, m[c], v[c]);
-            th[c] = t;
-            if (c >= n) m[c] = v[c] = 0.0f;               // places that do not exist count for nothing
-            top_m = max(top_m, __float_as_int(m[c]) & 0x7FFFFFFF);
-            top_v = max(top_v, __float_as_int(v[c]) & 0x7FFFFFFF);
+        for (int i = 0; i < STEP; ++i) {
+            g[i] = load_grad<B16>(A.grad, place(i), exist(i));
+            th[i] = sl_load_edge(A.theta + place(i), exist(i));
+            cm[i] = load_codes(A.m8 + place(i), exist(i)), cv[i] = load_codes(A.v8 + place(i), exist(i));
+            sm[i] = block_scale(A.ms[block(i)]), sv[i] = block_scale(A.vs[block(i)]);
         }
-        const unsigned xm = scale_byte(sl_wave_max(top_m)), xv = scale_byte(sl_wave_max(top_v));
-        const float im = __uint_as_float((254u - min(xm, 253u)) << 23), iv = __uint_as_float((254u - min(xv, 253u)) << 23);
-        const unsigned key = fmix(A.seed_hash ^ (unsigned)block);
-        unsigned om = 0, ov = 0;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const unsigned h = fmix(key ^ (unsigned)(lane * 4 + c));
-            om |= encode_m(m[c], im, (h & 0xFFFFu) << 4 | 8u) << (8 * c);
-            ov |= encode_v(v[c], iv, (h >> 16) << 4 | 8u) << (8 * c);
+        for (int i = 0; i < STEP; ++i) {
+            const int n = exist(i);
+            float m[4], v[4];
+            int top_m = 0, top_v = 0;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                m[c] = decode_m(cm[i] >> (8 * c) & 255u, sm[i]);
+                v[c] = decode_v(cv[i] >> (8 * c) & 255u, sv[i]);
+                float t = th[i][c];
+                adamw_update(A, keep, scale, g[i][c], t, m[c], v[c]);
+                th[i][c] = t;
+                if (c >= n) m[c] = v[c] = 0.0f;           // places that do not exist count for nothing
+                top_m = max(top_m, __float_as_int(m[c]) & 0x7FFFFFFF);
+                top_v = max(top_v, __float_as_int(v[c]) & 0x7FFFFFFF);
+            }
+            const unsigned xm = scale_byte(sl_wave_max(top_m)), xv = scale_byte(sl_wave_max(top_v));
+            const float im = __uint_as_float((254u - min(xm, 253u)) << 23), iv = __uint_as_float((254u - min(xv, 253u)) << 23);
+            const unsigned key = fmix(A.seed_hash ^ (unsigned)block(i));
+            unsigned om = 0, ov = 0;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const unsigned h = fmix(key ^ (unsigned)(lane * 4 + c));
+                om |= encode_m(m[c], im, (h & 0xFFFFu) << 4 | 8u) << (8 * c);
+                ov |= encode_v(v[c], iv, (h >> 16) << 4 | 8u) << (8 * c);
+            }
+            if (xm == 255u) om = 0;
+            if (xv == 255u) ov = 0;
+            sl_store_edge(A.theta + place(i), n, th[i]);
+            store_codes(A.m8 + place(i), n, om);
+            store_codes(A.v8 + place(i), n, ov);
+            if (A.theta16) store_bf16(A.theta16 + place(i), n, th[i]);
+            if (lane == 0 && has(i)) A.ms[block(i)] = (unsigned char)xm, A.vs[block(i)] = (unsigned char)xv;
         }
-        if (xm == 255u) om = 0;
-        if (xv == 255u) ov = 0;
-        sl_store_edge(A.theta + p, n, th);
-        store_codes(A.m8 + p, n, om);
-        store_codes(A.v8 + p, n, ov);
-        if (A.theta16) store_bf16(A.theta16 + p, n, th);
-        if (lane == 0) A.ms[block] = (unsigned char)xm, A.vs[block] = (unsigned char)xv;
-    }
+    };
+    if (u.count == UNIT) all(std::true_type{});
+    else all(std::false_type{});
 }
 
 template <bool V>
@@ -268,21 +313,37 @@ SL_DEV double group_sum(double x)
     return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-// fp64: the square of an fp32 number and its sums neither overflow nor vanish there.
+// fp64: the square of an fp32 number and its sums neither overflow nor vanish there.  A workgroup takes NORM_UNITS consecutive
+// units at a time, all of them requested before the first is added: 8 accesses of 16 bytes per lane in flight (bf16), where one unit
+// at a time reads 64M bf16 in 35 us and the 1.8B list in 677, this 24.6 and 530 to 553 (6.6 to 6.9 TB/s).
 template <bool B16>
 __global__ void __launch_bounds__(256) k_norm_parts(const Unit *units, long long n_units, const void *grad, double *parts)
 {
     double sum = 0.0;
-    for (long long t = blockIdx.x; t < n_units; t += gridDim.x) {
-        const Unit u = units[t];
+    for (long long t0 = (long long)blockIdx.x * NORM_UNITS; t0 < n_units; t0 += (long long)gridDim.x * NORM_UNITS) {
+        SlOctet<B16> g[NORM_UNITS][UNIT / 2048];
 #pragma unroll
-        for (int i = 0; i < UNIT / 1024; ++i) {
-            const int at = i * 1024 + (int)threadIdx.x * 4, n = u.count - at;
-            if (n <= 0) break;
-            const sl_f4 g = load_grad<B16>(grad, u.base + at, n);
-            const double x = g.x, y = g.y, z = g.z, w = g.w;
-            sum += (x * x + y * y) + (z * z + w * w);
+        for (int k = 0; k < NORM_UNITS; ++k) {
+            const Unit u = units[min(t0 + k, n_units - 1)];
+            const int count = t0 + k < n_units ? u.count : 0;
+#pragma unroll
+            for (int i = 0; i < UNIT / 2048; ++i) {
+                const int at = i * 2048 + (int)threadIdx.x * 8;
+                g[k][i].load(grad, u.base + at, count - at);
+            }
         }
+#pragma unroll
+        for (int k = 0; k < NORM_UNITS; ++k)
+#pragma unroll
+            for (int i = 0; i < UNIT / 2048; ++i) {
+                double s[8];
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    const double x = g[k][i].value(c);
+                    s[c] = x * x;
+                }
+                sum += ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+            }
     }
     sum = group_sum(sum);
     if (threadIdx.x == 0) parts[blockIdx.x] = sum;
@@ -431,7 +492,7 @@ int sl_grad_norm(sl_adamw *o, const void *grad, int grad_type, float max_norm, f
     if (const int rc = check_device(o)) return rc;
     hipStream_t st = static_cast<hipStream_t>(stream);
     double *parts = static_cast<double *>(workspace);
-    const int groups = (int)std::min<int64_t>(o->n_units, NORM_GROUPS);
+    const int groups = (int)std::min<int64_t>((o->n_units + NORM_UNITS - 1) / NORM_UNITS, NORM_GROUPS);
     if (groups > 0)
         hipLaunchKernelGGL(grad_type == SL_TYPE_BF16 ? k_norm_parts<true> : k_norm_parts<false>, dim3(groups), dim3(256), 0, st,
                            o->d_units, (long long)o->n_units, grad, parts);
@@ -455,8 +516,10 @@ int sl_adamw_step(sl_adamw *o, float *theta, const void *grad, int grad_type, fl
     if (o->n_units == 0) return SL_OK;
     A.units = o->d_units, A.theta = theta, A.grad = grad, A.m = m, A.v = v, A.grad_scale = grad_scale;
     A.theta16 = static_cast<unsigned short *>(theta16);
-    hipLaunchKernelGGL(grad_type == SL_TYPE_BF16 ? k_adamw<true> : k_adamw<false>, dim3((unsigned)o->n_units), dim3(256), 0,
-                       static_cast<hipStream_t>(stream), A);
+    A.order = (unsigned)o->n_units / SL_ORDER_WINDOW * SL_ORDER_WINDOW;
+    const bool b16 = grad_type == SL_TYPE_BF16, is_short = o->n_units < SHORT_UNITS;
+    hipLaunchKernelGGL(is_short ? (b16 ? k_adamw<true, true> : k_adamw<false, true>) : (b16 ? k_adamw<true, false> : k_adamw<false, false>),
+                       dim3((unsigned)o->n_units), dim3(256), is_short ? 0 : STREAM_LDS, static_cast<hipStream_t>(stream), A);
     return check_launch();
 }
 
@@ -478,11 +541,13 @@ int sl_adamw_step8(sl_adamw *o, float *theta, const void *grad, int grad_type, u
     if (const int rc = check_device(o)) return rc;
     if (o->n_units == 0) return SL_OK;
     A.units = o->d_units, A.theta = theta, A.grad = grad, A.grad_scale = grad_scale;
+    A.order = (unsigned)o->n_units / SL_ORDER_WINDOW * SL_ORDER_WINDOW;
     A.m8 = m_codes, A.v8 = v_codes, A.ms = m_scales, A.vs = v_scales;
     A.seed_hash = host_fmix(seed);
     A.theta16 = static_cast<unsigned short *>(theta16);
-    hipLaunchKernelGGL(grad_type == SL_TYPE_BF16 ? k_adamw8<true> : k_adamw8<false>, dim3((unsigned)o->n_units), dim3(256), 0,
-                       static_cast<hipStream_t>(stream), A);
+    const bool b16 = grad_type == SL_TYPE_BF16, is_short = o->n_units < SHORT_UNITS;
+    hipLaunchKernelGGL(is_short ? (b16 ? k_adamw8<true, true> : k_adamw8<false, true>) : (b16 ? k_adamw8<true, false> : k_adamw8<false, false>),
+                       dim3((unsigned)o->n_units), dim3(256), is_short ? 0 : STREAM8_LDS, static_cast<hipStream_t>(stream), A);
     return check_launch();
 }
 

@@ -106,6 +106,11 @@ struct SlOctet {
             }
         }
     }
+    SL_DEV float value(int i) const
+    {
+        if constexpr (B16) return __uint_as_float(i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
+        else return __uint_as_float(w[i]);
+    }
     // fp32 bits of the largest magnitude
     SL_DEV unsigned top() const
     {
