@@ -432,7 +432,7 @@ int sl_adamw_state_values(sl_adamw *opt, int moment, const uint8_t *codes, const
  * in tiles of 64 rows x 128 columns - the byte of block b of row r is at 128*(b mod 2) + 4*(r mod 32)
  * + 2*(r/32) + b/2.
  * Rows and columns that fill up tiles are zero.  sl_mx4_bytes() is the size (0 for a size that is not
- * positive or has more than 2^24 tiles of codes); 16-byte aligned. */
+ * positive or has more than 2^22 tiles of codes); 16-byte aligned. */
 size_t sl_mx4_bytes(int64_t rows, int64_t cols);
 
 /* src     in,  device, rows x cols of src_type, row r at element r*ld (ld >= cols), aligned to its element

@@ -114,26 +114,27 @@ __global__ void __launch_bounds__(256) k_quantize(QuantArgs A)
     }
 }
 
-// Eight elements - a word of codes - in a lane, 16 lanes to a row of a tile.
-template <bool B16>
-__global__ void __launch_bounds__(256) k_dequantize(const unsigned char *q, SlMx4Shape s, void *out, long long ld)
+// Eight elements - a word of codes - in a lane, 512 columns of a row in a wave, 16 rows in a workgroup: rows are written in pieces
+// of 1 KB (in pieces of 256 bytes, neighbours meet in the lines at the ends of unaligned ones: 2048 x 50,257 bf16 89 us, so 63).
+// HINT: streaming stores, for rows that begin on 16 bytes (50,257 x 2048 53 us without, 38 with).
+template <bool B16, bool HINT>
+__global__ void __launch_bounds__(256) k_dequantize(const unsigned char *q, SlMx4Shape s, void *out, long long ld, long long col_groups)
 {
     typedef unsigned u4a __attribute__((ext_vector_type(4), aligned(2)));
-    const int octet = threadIdx.x & 15, sub = threadIdx.x >> 4, b = octet >> 2;
-    const long long rg = blockIdx.x / s.col_tiles, kt = blockIdx.x % s.col_tiles;
-    const long long col = kt * MX_COLS + octet * 8;
+    const int lane = threadIdx.x & 63, wave = sl_uniform((int)(threadIdx.x >> 6)), b = lane >> 2 & 3;
+    const long long row0 = blockIdx.x / col_groups * 16 + wave * 4, col = blockIdx.x % col_groups * 512 + lane * 8;
     const int n = (int)max(min(s.cols - col, 8ll), 0ll);
-    const unsigned char *scales = q + s.scales + (rg * s.col_tiles + kt) * MX_SCALE_TILE_BYTES;
+    const long long kt = min(col / MX_COLS, s.col_tiles - 1);
     unsigned code[4], byte[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const long long rt = min(rg * 2 + i / 2, s.row_tiles - 1);
-        code[i] = *reinterpret_cast<const unsigned *>(q + (rt * s.col_tiles + kt) * MX_TILE_BYTES + sl_mx4_code_at((i & 1) * 16 + sub, b) + (octet & 3) * 4);
-        byte[i] = scales[sl_mx4_scale_at(i * 16 + sub, b)];
+        const long long row = min(row0 + i, s.rows - 1);
+        code[i] = *reinterpret_cast<const unsigned *>(q + (row / MX_ROWS * s.col_tiles + kt) * MX_TILE_BYTES + sl_mx4_code_at((int)(row & 31), b) + (lane & 3) * 4);
+        byte[i] = q[s.scales + (row / MX_SCALE_ROWS * s.col_tiles + kt) * MX_SCALE_TILE_BYTES + sl_mx4_scale_at((int)(row & 63), b)];
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const long long row = rg * 64 + i * 16 + sub;
+        const long long row = row0 + i;
         if (row >= s.rows) return;
         const unsigned x = byte[i];
         const float f = sl_mx4_factor(x);
@@ -146,11 +147,15 @@ __global__ void __launch_bounds__(256) k_dequantize(const unsigned char *q, SlMx
             for (int j = 0; j < 8; ++j) e[j] = f;
         }
         const long long at = row * ld + col;
+        auto put = [&](void *to, sl_u4 w) __attribute__((always_inline)) {
+            if constexpr (HINT) __builtin_nontemporal_store(w, static_cast<sl_u4 *>(to));
+            else *static_cast<u4a *>(to) = w;
+        };
         if constexpr (B16) {
             unsigned short *o = static_cast<unsigned short *>(out) + at;
             const sl_u4 w = {sl_bf16_pair(e[0], e[1]), sl_bf16_pair(e[2], e[3]), sl_bf16_pair(e[4], e[5]), sl_bf16_pair(e[6], e[7])};
             if (n >= 8) {
-                *reinterpret_cast<u4a *>(o) = w;
+                put(o, w);
             } else {
 #pragma unroll
                 for (int j = 0; j < 7; ++j)
@@ -159,9 +164,8 @@ __global__ void __launch_bounds__(256) k_dequantize(const unsigned char *q, SlMx
         } else {
             float *o = static_cast<float *>(out) + at;
             if (n >= 8) {
-                typedef float f4a __attribute__((ext_vector_type(4), aligned(4)));
-                *reinterpret_cast<f4a *>(o) = sl_f4{e[0], e[1], e[2], e[3]};
-                *reinterpret_cast<f4a *>(o + 4) = sl_f4{e[4], e[5], e[6], e[7]};
+                put(o, sl_u4{__float_as_uint(e[0]), __float_as_uint(e[1]), __float_as_uint(e[2]), __float_as_uint(e[3])});
+                put(o + 4, sl_u4{__float_as_uint(e[4]), __float_as_uint(e[5]), __float_as_uint(e[6]), __float_as_uint(e[7])});
             } else {
 #pragma unroll
                 for (int j = 0; j < 7; ++j)
@@ -232,9 +236,12 @@ int sl_mx4_dequantize(const void *q, int64_t rows, int64_t cols, void *out, int 
     if (!q || !out || q == out || !sl_mx4_shape(rows, cols, s)) return SL_ERR_INVALID_ARG;
     if (out_type != SL_TYPE_F32 && out_type != SL_TYPE_BF16) return SL_ERR_INVALID_ARG;
     if (ld < cols || ld > ((int64_t)1 << 40) || misaligned(q, 16) || misaligned(out, out_type == SL_TYPE_BF16 ? 2 : 4)) return SL_ERR_INVALID_ARG;
-    const dim3 grid((unsigned)((s.row_tiles + 1) / 2 * s.col_tiles));
-    hipLaunchKernelGGL(out_type == SL_TYPE_BF16 ? k_dequantize<true> : k_dequantize<false>, grid, dim3(256), 0,
-                       static_cast<hipStream_t>(stream), static_cast<const unsigned char *>(q), s, out, (long long)ld);
+    // (fp32: a lane's two pieces of 16 bytes would go to memory one by one)
+    const bool b16 = out_type == SL_TYPE_BF16, hint = b16 && !misaligned(out, 16) && (ld & 7) == 0;
+    const long long col_groups = (cols + 511) / 512;
+    const dim3 grid((unsigned)((rows + 15) / 16 * col_groups));
+    hipLaunchKernelGGL((b16 ? (hint ? k_dequantize<true, true> : k_dequantize<true, false>) : k_dequantize<false, false>), grid, dim3(256), 0,
+                       static_cast<hipStream_t>(stream), static_cast<const unsigned char *>(q), s, out, (long long)ld, col_groups);
     return check_launch();
 }
 

@@ -381,7 +381,7 @@ bool misaligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0;
 
 const int64_t LONGEST = (int64_t)1 << 40;
 
-// (with m n <= 2^36 and at most 2^29 rows each, tiles of 128 x 128 are less than 2^24)
+// (with m n <= 2^36 and at most 2^27 rows each, tiles of 128 x 128 are less than 2^24: a grid has less than 2^32 threads)
 bool bad_sizes(int64_t m, int64_t n, int64_t k)
 {
     if (m < 0 || n < 0 || k < 0) return true;
@@ -468,9 +468,8 @@ int product(const unsigned char *a, const unsigned char *b, int64_t m, int64_t n
 int64_t few_rows_lds(int64_t m, int64_t k) { return 8 * 1024 + (k + MX_COLS - 1) / MX_COLS * m * 68; }
 
 // Where it is not quicker to quantise x once, in a launch of its own: up to 640 steps of 128 in x's rows together (us, this kernel / two
-// launches: 8 rows, k = 8192 9.9 / 14.8, 16 rows, k = 2048 6.6 / 8.6, 16 rows, k = 8192 22.5 / 14.8).  That is at most 52 KB of LDS;
-// and a grid has less than 2^32 threads.
-bool few_rows(int64_t m, int64_t n, int64_t k) { return m <= 16 && m * ((k + MX_COLS - 1) / MX_COLS) <= 640 && n <= (1 << 26); }
+// launches: 8 rows, k = 8192 9.9 / 14.8, 16 rows, k = 2048 6.6 / 8.6, 16 rows, k = 8192 22.5 / 14.8).  That is at most 52 KB of LDS.
+bool few_rows(int64_t m, int64_t k) { return m <= 16 && m * ((k + MX_COLS - 1) / MX_COLS) <= 640; }
 
 template <bool X16, bool Y16>
 int launch_few_rows(const FewArgs &A, int64_t lds, hipStream_t st)
@@ -497,7 +496,7 @@ size_t sl_mx4_workspace_bytes(int64_t m, int64_t n, int64_t k)
 {
     if (bad_sizes(m, n, k) || m == 0 || n == 0 || k == 0) return 0;
     const int parts = choose(m, n, k).parts;
-    return (few_rows(m, n, k) ? 0 : align256(sl_mx4_bytes(m, k))) + (parts > 1 ? parts * sizeof(float) * (size_t)(m * part_pitch(n)) : 0);
+    return (few_rows(m, k) ? 0 : align256(sl_mx4_bytes(m, k))) + (parts > 1 ? parts * sizeof(float) * (size_t)(m * part_pitch(n)) : 0);
 }
 
 int sl_mx4_product(const void *a, const void *b, int64_t m, int64_t n, int64_t k, void *c, int c_type, int64_t ldc,
@@ -526,7 +525,7 @@ int sl_mx4_linear(const void *x, int x_type, int64_t ldx, const void *w, int64_t
         return SL_ERR_INVALID_ARG;
     if (!workspace && sl_mx4_workspace_bytes(m, n, k)) return SL_ERR_INVALID_ARG;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (k > 0 && few_rows(m, n, k)) {
+    if (k > 0 && few_rows(m, k)) {
         FewArgs A;
         A.x = x, A.ldx = ldx, A.w = static_cast<const unsigned char *>(w), A.m = (int)m, A.y = y, A.ldy = ldy;
         (void)sl_mx4_shape(n, k, A.s);
