@@ -415,23 +415,29 @@ Choice choose(int64_t m, int64_t n, int64_t k)
 long long part_pitch(int64_t n) { return (n + 3) / 4 * 4; }
 
 template <bool B16, int TM, int TN, int STAGES, int WGS>
-void launch_tiles(ProductArgs A, int parts, hipStream_t st)
+int launch_tiles(ProductArgs A, int parts, hipStream_t st)
 {
     A.m_tiles = (A.m + 64 * TM - 1) / (64 * TM);
     A.n_tiles = (A.n + 64 * TN - 1) / (64 * TN);
     constexpr unsigned bytes = STAGES * ((2 * TM + 2 * TN) * MX_TILE_BYTES + 2048);
-    static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_product<B16, TM, TN, STAGES, WGS>),
-                                                          hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    (void)allowed;
+    if (bytes > 65536) {
+        const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_product<B16, TM, TN, STAGES, WGS>),
+                                                   hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        if (err != hipSuccess) {
+            sl_note_hip_error(err);
+            return SL_ERR_HIP;
+        }
+    }
     hipLaunchKernelGGL((k_product<B16, TM, TN, STAGES, WGS>), dim3((unsigned)(A.m_tiles * A.n_tiles * parts)), dim3(256), bytes, st, A);
+    return check_launch();
 }
 
 template <bool B16>
-void launch(const ProductArgs &A, Choice c, hipStream_t st)
+int launch(const ProductArgs &A, Choice c, hipStream_t st)
 {
-    if (c.tile == 0) launch_tiles<B16, 1, 1, 4, 4>(A, c.parts, st);
-    else if (c.tile == 1) launch_tiles<B16, 2, 2, 4, 2>(A, c.parts, st);
-    else launch_tiles<B16, 2, 4, 3, 2>(A, c.parts, st);
+    return c.tile == 0 ? launch_tiles<B16, 1, 1, 4, 4>(A, c.parts, st)
+         : c.tile == 1 ? launch_tiles<B16, 2, 2, 4, 2>(A, c.parts, st)
+                       : launch_tiles<B16, 2, 4, 3, 2>(A, c.parts, st);
 }
 
 // parts: room for the results of the parts of the contraction
@@ -450,15 +456,12 @@ int product(const unsigned char *a, const unsigned char *b, int64_t m, int64_t n
     A.a_scales = sa.scales, A.b_scales = sb.scales;
     A.m = m, A.n = n, A.c = c, A.ldc = ldc, A.accumulate = accumulate;
     A.part_steps = (A.k_tiles + how.parts - 1) / how.parts, A.part_size = 0;
-    if (how.parts == 1) {
-        if (type == SL_TYPE_BF16) launch<true>(A, how, st);
-        else launch<false>(A, how, st);
-        return check_launch();
-    }
+    if (how.parts == 1)
+        return type == SL_TYPE_BF16 ? launch<true>(A, how, st) : launch<false>(A, how, st);
     ProductArgs P = A;
     const long long ldp = part_pitch(n);
     P.c = parts, P.ldc = ldp, P.part_size = A.part_size = m * ldp, P.accumulate = 0;
-    launch<false>(P, how, st);
+    if (const int rc = launch<false>(P, how, st)) return rc;
     const dim3 grid((unsigned)((m * (ldp / 4) + 255) / 256));
     hipLaunchKernelGGL(type == SL_TYPE_BF16 ? k_join<true> : k_join<false>, grid, dim3(256), 0, st, A, parts, ldp, how.parts);
     return check_launch();
