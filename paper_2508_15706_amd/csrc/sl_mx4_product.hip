@@ -399,16 +399,20 @@ struct Choice {
 //   few: every one gets a tile as soon as they are small - 1024 x 1024 x 4096 7.3 / 11.0 / 17.8, 256 x 8192 x 2048 7.0 / 7.8 / 11.6 -
 //   until 64 x 64 are more than two to a compute unit: 1024 x 4096 x 1024 8.8 / 6.8 / 9.1, 2048 cubed 11.8 / 8.7 / 12.5;
 //   many: the larger tile reads LDS less for the same products, and power is what bounds them: 4096 x 2048 x 2048 (512 of 128 x 128)
-//   21.5 / 13.8 / 14.9, 4096 x 4096 x 1024 (1024) 26.6 / 17.4 / 17.1, 16,384 x 2048 x 8192 (2048) - / 141 / 128.
-// A long contraction on very few tiles is cut into parts of 16 steps or more, whose results a second launch adds: 100 x 1000 x 16,384
-// (32 tiles) 19.4 whole, 9.9 in eight parts; from 128 tiles on it gains nothing (256 x 2048 x 8192 11.4 and 11.6 in two).
+//   21.5 / 13.8 / 14.9, 8575 x 1866 x 3815 (1005) 72 / 41 / 48, 7835 x 2305 x 2599 (1178) 59 / 37.4 / 38.2, 517 x 50,257 x 2048 (1965)
+//   72 / 46 / 40.5, 16,384 x 2048 x 8192 (2048) - / 141 / 128.
+// A long contraction on very few tiles is cut into parts of 12 steps or more, whose results a second launch adds: 100 x 1000 x 16,384
+// (32 tiles, 128 steps) 19.4 whole, 9.9 in eight parts; 55 x 613 x 6252 (10 tiles, 49 steps) 8.9, 7.4 in four; 2378 x 67 x 11,212 (76 tiles)
+// 15.1, 11.8 in four; from 128 tiles on it gains nothing (256 x 2048 x 8192 11.4 and 11.6 in two).
+// (Over 60 sizes drawn from 16 .. 16,384 x 16 .. 8192 x 16 .. 16,384 the rule's choice takes 1 to 2 % longer than the best of the three sizes in
+// one, two, four or eight parts.)
 Choice choose(int64_t m, int64_t n, int64_t k)
 {
     const int64_t small = ((m + 63) / 64) * ((n + 63) / 64), middle = ((m + 127) / 128) * ((n + 127) / 128), steps = (k + MX_COLS - 1) / MX_COLS;
-    if (middle > 768) return Choice{2, 1};
+    if (middle > 1280) return Choice{2, 1};
     if (small > 576) return Choice{1, 1};
-    if (small > 64 || steps < 64) return Choice{0, 1};
-    const int64_t per = std::max<int64_t>(16, (steps + 7) / 8);
+    if (small > 96 || steps < 36) return Choice{0, 1};
+    const int64_t per = std::max<int64_t>({12, (steps + 7) / 8, (steps * small + 255) / 256});
     return Choice{0, (int)((steps + per - 1) / per)};
 }
 
