@@ -395,12 +395,18 @@ struct Choice {
     int parts;                           // of the contraction
 };
 
+// Tenths of a round (see below) that so many of the larger tiles take.
+int64_t rounds10(int64_t tiles) { return tiles / 512 * 10 + (tiles % 512 == 0 ? 0 : tiles % 512 <= 256 ? 6 : 10); }
+
 // By how many tiles there are for the 256 compute units (us, 64 x 64 / 128 x 128 / 128 x 256):
 //   few: every one gets a tile as soon as they are small - 1024 x 1024 x 4096 7.3 / 11.0 / 17.8, 256 x 8192 x 2048 7.0 / 7.8 / 11.6 -
-//   until 64 x 64 are more than two to a compute unit: 1024 x 4096 x 1024 8.8 / 6.8 / 9.1, 2048 cubed 11.8 / 8.7 / 12.5;
-//   many: the larger tile reads LDS less for the same products, and power is what bounds them: 4096 x 2048 x 2048 (512 of 128 x 128)
-//   21.5 / 13.8 / 14.9, 8575 x 1866 x 3815 (1005) 72 / 41 / 48, 7835 x 2305 x 2599 (1178) 59 / 37.4 / 38.2, 517 x 50,257 x 2048 (1965)
-//   72 / 46 / 40.5, 16,384 x 2048 x 8192 (2048) - / 141 / 128.
+//   until 64 x 64 are more than two to a compute unit: 2388 x 956 x 16,370 (570) 46 / 34 / 58, 1024 x 4096 x 1024 8.8 / 6.8 / 9.1, 2048 cubed
+//   11.8 / 8.7 / 12.5;
+//   many: 512 workgroups of either larger tile run at a time, two to a compute unit, and a round of 128 x 256 takes 1.75 times as long as one of
+//   128 x 128 (it reads LDS less for the same products, and power is what bounds them); up to 256 tiles that are left over run one to a unit,
+//   in 0.6 of a round.  So the rounds decide: 8192 x 2048 x 16,384 (512 and 1024 tiles) - / 138 / 128, 8575 x 1866 x 3815 (536 and 1005) 72 / 41 / 48,
+//   517 x 50,257 x 2048 (985 and 1965) 72 / 46 / 40.5, 12,688 x 1510 x 323 (600 and 1200) 21.4 / 15.6 / 16.4, 5054 x 4236 x 5982 (680 and 1360)
+//   124 / 77 / 72.
 // A long contraction on very few tiles is cut into parts of 12 steps or more, whose results a second launch adds: 100 x 1000 x 16,384
 // (32 tiles, 128 steps) 19.4 whole, 9.9 in eight parts; 55 x 613 x 6252 (10 tiles, 49 steps) 8.9, 7.4 in four; 2378 x 67 x 11,212 (76 tiles)
 // 15.1, 11.8 in four; from 128 tiles on it gains nothing (256 x 2048 x 8192 11.4 and 11.6 in two).
@@ -408,11 +414,11 @@ struct Choice {
 // one, two, four or eight parts.)
 Choice choose(int64_t m, int64_t n, int64_t k)
 {
-    const int64_t small = ((m + 63) / 64) * ((n + 63) / 64), middle = ((m + 127) / 128) * ((n + 127) / 128), steps = (k + MX_COLS - 1) / MX_COLS;
-    if (middle > 1280) return Choice{2, 1};
-    if (small > 576) return Choice{1, 1};
-    if (small > 96 || steps < 36) return Choice{0, 1};
-    const int64_t per = std::max<int64_t>({12, (steps + 7) / 8, (steps * small + 255) / 256});
+    const int64_t small = ((m + 63) / 64) * ((n + 63) / 64), middle = ((m + 127) / 128) * ((n + 127) / 128),
+                  large = ((m + 127) / 128) * ((n + 255) / 256), steps = (k + MX_COLS - 1) / MX_COLS;
+    if (small > 512) return Choice{7 * rounds10(large) < 4 * rounds10(middle) ? 2 : 1, 1};
+    if (small > 100 || steps < 36) return Choice{0, 1};
+    const int64_t per = std::max<int64_t>({12, (steps + 7) / 8, (steps * small + 383) / 384});
     return Choice{0, (int)((steps + per - 1) / per)};
 }
 
