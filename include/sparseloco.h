@@ -17,15 +17,21 @@
  * Indices travel as 12-bit fields, or Rice-coded (appendix "Compression of indices in
  * Top-k"): sl_compress_coded / sl_decompress_avg_apply_coded.
  *
+ * What a worker computes between two outer steps (Algorithm 1, inner loop) is here too:
+ * linear layers on microscaled 4-bit operands with both gradients (sl_mx4_*), the norm that
+ * the gradients are clipped by (sl_grad_norm) and AdamW (sl_adamw_*), see "The inner step".
+ *
  * Conventions for every function
  *   - returns SL_OK (0) or a negative sl_status; never throws, never aborts;
  *   - arguments are validated on the host before anything is enqueued; on an
  *     argument error nothing is launched and no buffer is touched;
  *   - "device" pointers are HIP device memory of the device that was current
- *     when the plan was created; "host" pointers are ordinary host memory;
+ *     when the plan (sl_adamw) was created, of the current device where there is
+ *     neither; "host" pointers are ordinary host memory;
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream);
  *     kernels are enqueued on it and the call returns without synchronising;
- *   - the caller owns every buffer it passes; the library owns only sl_plan.
+ *   - the caller owns every buffer it passes; the library owns only sl_plan
+ *     and sl_adamw;
  *   - results are deterministic: the same inputs give the same bytes;
  *   - no environment variable is read.
  */
@@ -44,8 +50,9 @@ typedef enum {
     SL_ERR_INVALID_ARG = -1, /* null / misaligned pointer, bad k, R or shape        */
     SL_ERR_BAD_PAYLOAD = -2, /* sl_payload_validate found a malformed record        */
     SL_ERR_HIP = -3,         /* a HIP runtime call failed; see sl_last_hip_error()  */
-    SL_ERR_NOMEM = -4,       /* host or device allocation failed (plan creation)    */
-    SL_ERR_DEVICE = -5,      /* current device differs from the plan's device       */
+    SL_ERR_NOMEM = -4,       /* host or device allocation failed (plan creation,
+                                sl_adamw_create)                                   */
+    SL_ERR_DEVICE = -5,      /* current device differs from the plan's (sl_adamw's) */
     SL_ERR_TOO_LARGE = -6    /* sl_compress_noalloc: the plan needs more scratch
                                 than SL_NOALLOC_SCRATCH_BYTES                      */
 } sl_status;

@@ -509,18 +509,18 @@ def _type_of(t: torch.Tensor) -> int:
 
 def _matrix(t: torch.Tensor):
     """(pointer, type, rows, cols, row stride) of a device matrix whose rows are contiguous."""
-    if t.dim() != 2 or not t.is_cuda:
-        raise ValueError("expected a device matrix")
-    (rows, cols), (ld, step), typ = t.shape, t.stride(), _TYPES.get(t.dtype)
-    if typ is None:
-        raise ValueError(f"expected float32 or bfloat16, got {t.dtype}")
-    if step != 1 and cols > 1:
-        raise ValueError("expected contiguous rows")
+    rows, cols = t.shape
+    ld, step = t.stride()
+    typ = _TYPES.get(t.dtype)
+    if typ is None or not t.is_cuda or (step != 1 and cols > 1):
+        raise ValueError("expected a float32 or bfloat16 device matrix with contiguous rows")
     return t.data_ptr(), typ, rows, cols, (ld if rows > 1 else max(cols, ld))
 
 
 def _mx4_ptr(q: Optional[torch.Tensor], rows: int, cols: int) -> Optional[int]:
-    if q is not None and q.numel() < sl_mx4_bytes(rows, cols):
+    if q is None:
+        return None
+    if q.numel() < sl_mx4_bytes(rows, cols):
         raise ValueError(f"a 4-bit matrix of {rows} x {cols} has {sl_mx4_bytes(rows, cols)} bytes, got {q.numel()}")
     return _dev_ptr(q, torch.uint8)
 
