@@ -445,7 +445,8 @@ size_t sl_mx4_bytes(int64_t rows, int64_t cols);
 /* src     in,  device, rows x cols of src_type, row r at element r*ld (ld >= cols), aligned to its element
  * q       out, device, sl_mx4_bytes(rows, cols): blocks along the rows, or NULL
  * qt      out, device, sl_mx4_bytes(cols, rows): the transposed matrix, blocks along src's columns, or
- *         NULL; at least one of the two.  Both come from one pass over src. */
+ *         NULL; at least one of the two.  Both come from one pass over src.
+ * A matrix without rows or columns (an empty batch) is nothing to do. */
 int sl_mx4_quantize(const void *src, int src_type, int64_t rows, int64_t cols, int64_t ld, void *q, void *qt,
                     void *stream);
 /* The values of q, each rounded once where the type is bf16 and its exponent is out of range. */

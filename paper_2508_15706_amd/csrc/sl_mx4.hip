@@ -221,6 +221,8 @@ size_t sl_mx4_bytes(int64_t rows, int64_t cols)
 int sl_mx4_quantize(const void *src, int src_type, int64_t rows, int64_t cols, int64_t ld, void *q, void *qt, void *stream)
 {
     SlMx4Shape s, t;
+    if (rows < 0 || cols < 0) return SL_ERR_INVALID_ARG;
+    if (rows == 0 || cols == 0) return SL_OK;
     if (!src || (!q && !qt) || q == qt || q == src || qt == src || !sl_mx4_shape(rows, cols, s) || !sl_mx4_shape(cols, rows, t))
         return SL_ERR_INVALID_ARG;
     if (src_type != SL_TYPE_F32 && src_type != SL_TYPE_BF16) return SL_ERR_INVALID_ARG;
@@ -233,6 +235,8 @@ int sl_mx4_quantize(const void *src, int src_type, int64_t rows, int64_t cols, i
 int sl_mx4_dequantize(const void *q, int64_t rows, int64_t cols, void *out, int out_type, int64_t ld, void *stream)
 {
     SlMx4Shape s;
+    if (rows < 0 || cols < 0) return SL_ERR_INVALID_ARG;
+    if (rows == 0 || cols == 0) return SL_OK;
     if (!q || !out || q == out || !sl_mx4_shape(rows, cols, s)) return SL_ERR_INVALID_ARG;
     if (out_type != SL_TYPE_F32 && out_type != SL_TYPE_BF16) return SL_ERR_INVALID_ARG;
     if (ld < cols || ld > ((int64_t)1 << 40) || misaligned(q, 16) || misaligned(out, out_type == SL_TYPE_BF16 ? 2 : 4)) return SL_ERR_INVALID_ARG;

@@ -35,6 +35,8 @@ def test_refusals_before_any_device_work():
     assert L.sl_mx4_quantize(a + 2, 0, 4, 4, 4, b, None, None) == -1
     assert L.sl_mx4_quantize(a, 0, 4, 4, 4, b, b, None) == -1
     assert L.sl_mx4_quantize(None, 0, 4, 4, 4, b, None, None) == -1
+    assert L.sl_mx4_quantize(a, 0, -1, 4, 4, b, None, None) == -1 and L.sl_mx4_dequantize(a, 4, -1, b, 1, 4, None) == -1
+    assert L.sl_mx4_quantize(None, 0, 0, 4, 4, b, None, None) == 0 and L.sl_mx4_dequantize(a, 4, 0, None, 1, 4, None) == 0   # nothing to do
     assert L.sl_mx4_quantize(a, 0, 1 << 40, 1 << 40, 1 << 40, b, None, None) == -1
     assert L.sl_mx4_dequantize(a, 4, 4, b, 1, 3, None) == -1
     assert L.sl_mx4_dequantize(a, 4, 4, a, 1, 4, None) == -1
