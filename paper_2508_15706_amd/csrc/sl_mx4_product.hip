@@ -38,6 +38,23 @@ SL_DEV sl_f16 mx4_step(sl_u4 b, sl_u4 a, sl_f16 c, unsigned sb, unsigned sa)
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, OB, (int)sb, OA, (int)sa);
 }
 
+// Four columns of a row of an fp32 c; those that do not exist are zero.
+SL_DEV sl_f4 load_piece(const ProductArgs &A, long long row, long long col)
+{
+    typedef float f4a __attribute__((ext_vector_type(4), aligned(4)));
+    const long long n = row < A.m ? A.n - col : 0;
+    const float *c = static_cast<const float *>(A.c) + row * A.ldc + col;
+    sl_f4 v = {0.f, 0.f, 0.f, 0.f};
+    if (n >= 4) {
+        v = *reinterpret_cast<const f4a *>(c);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (i < n) v[i] = c[i];
+    }
+    return v;
+}
+
 // 16 bytes of a row of c: eight columns of bf16, four of fp32.
 template <bool B16>
 SL_DEV void store_piece(const ProductArgs &A, unsigned part, long long row, long long col, sl_u4 w)
@@ -55,17 +72,14 @@ SL_DEV void store_piece(const ProductArgs &A, unsigned part, long long row, long
                 if (i < n) c[i] = (unsigned short)(w[i >> 1] >> (16 * (i & 1)));
         }
     } else {
-        typedef float f4a __attribute__((ext_vector_type(4), aligned(4)));
-        float *c = static_cast<float *>(A.c) + at;
-        sl_f4 v = {__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w)};
+        typedef unsigned u4a __attribute__((ext_vector_type(4), aligned(4)));
+        unsigned *c = static_cast<unsigned *>(A.c) + at;
         if (n >= 4) {
-            f4a *p = reinterpret_cast<f4a *>(c);
-            if (A.accumulate) v = v + (sl_f4)*p;
-            *p = v;
+            *reinterpret_cast<u4a *>(c) = w;
         } else {
 #pragma unroll
             for (int i = 0; i < 3; ++i)
-                if (i < n) c[i] = A.accumulate ? c[i] + v[i] : v[i];
+                if (i < n) c[i] = w[i];
         }
     }
 }
@@ -87,8 +101,7 @@ SL_DEV TilePlace tile_place(unsigned i, unsigned tiles, long long m_tiles, long 
 
 // 16 (scales: the same) bytes per lane from memory to LDS at `lds` + 16 * lane, past the registers.  The instruction is
 // written out because the compiler, which cannot tell the stages apart, would wait for all of them before every read
-// of LDS; it has no result in a register, the waits for it are
-// written out too, and nothing else in these kernels uses m0.
+// of LDS; it has no result in a register, the waits for it are written out too, and nothing else in these kernels uses m0.
 SL_DEV void dma16(const unsigned char *base, unsigned lane_off, unsigned lds)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(lane_off), "s"(base) : "memory");
@@ -230,7 +243,8 @@ __global__ void __launch_bounds__(256, WGS) k_product(ProductArgs A)
     }
     // c through LDS, 32 rows of a wave at a time, so that a row's columns are written in one piece
     __syncthreads();
-    constexpr int PITCH = TN * 32 * (B16 ? 2 : 4) + 16, PIECES = TN * 32 * (B16 ? 2 : 4) / 16;
+    constexpr int PITCH = TN * 32 * (B16 ? 2 : 4) + 16, PIECES = TN * 32 * (B16 ? 2 : 4) / 16, TOGETHER = PIECES < 8 ? PIECES / 2 : 4;
+    static_assert(PIECES / 2 % TOGETHER == 0, "whole groups of pieces");
     unsigned char *mine = lds + wave * (32 * PITCH);
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
@@ -250,10 +264,24 @@ __global__ void __launch_bounds__(256, WGS) k_product(ProductArgs A)
             }
         sl_wave_sync();
         const long long row0 = (i0 + wm * TM + i) * MX_ROWS, col0 = (j0 + wn * TN) * MX_ROWS;
+        // (four pieces at a time: what c already holds, where it is added to, is requested together)
 #pragma unroll
-        for (int t = 0; t < PIECES / 2; ++t) {
-            const int piece = t * 64 + lane, row = piece / PIECES, at = piece % PIECES;
-            store_piece<B16>(A, part, row0 + row, col0 + at * (B16 ? 8 : 4), *reinterpret_cast<const sl_u4 *>(mine + row * PITCH + at * 16));
+        for (int t = 0; t < PIECES / 2; t += TOGETHER) {
+            sl_f4 there[TOGETHER];
+            if (!B16 && A.accumulate) {
+#pragma unroll
+                for (int u = 0; u < TOGETHER; ++u) {
+                    const int piece = (t + u) * 64 + lane, row = piece / PIECES, at = piece % PIECES;
+                    there[u] = load_piece(A, row0 + row, col0 + at * 4);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < TOGETHER; ++u) {
+                const int piece = (t + u) * 64 + lane, row = piece / PIECES, at = piece % PIECES;
+                sl_u4 w = *reinterpret_cast<const sl_u4 *>(mine + row * PITCH + at * 16);
+                if (!B16 && A.accumulate) w = __builtin_bit_cast(sl_u4, there[u] + __builtin_bit_cast(sl_f4, w));
+                store_piece<B16>(A, part, row0 + row, col0 + at * (B16 ? 8 : 4), w);
+            }
         }
         sl_wave_sync();
     }
