@@ -351,8 +351,14 @@ __global__ void __launch_bounds__(256) k_norm_parts(const Unit *units, long long
 
 __global__ void __launch_bounds__(256) k_norm_result(const double *parts, int n, float max_norm, float *result)
 {
-    double sum = 0.0;
-    for (int i = threadIdx.x; i < n; i += 256) sum += parts[i];
+    double part[NORM_GROUPS / 256], sum = 0.0;
+#pragma unroll
+    for (int k = 0; k < NORM_GROUPS / 256; ++k) {              // (all requested at once)
+        const int i = k * 256 + (int)threadIdx.x;
+        part[k] = i < n ? parts[i] : 0.0;
+    }
+#pragma unroll
+    for (int k = 0; k < NORM_GROUPS / 256; ++k) sum += part[k];
     sum = group_sum(sum);
     if (threadIdx.x == 0) {
         const double norm = sqrt(sum);
