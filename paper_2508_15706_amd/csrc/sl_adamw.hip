@@ -2,12 +2,12 @@
 // the gradients.  All of it is streams over flat arenas, bound by memory: a unit is up to 4096 consecutive elements
 // of one tensor and belongs to one workgroup of four waves, wave w of which takes elements 1024 i + 256 w .. + 255 in
 // access i - one block of the 8-bit states, whose largest value is then a maximum over the wave's registers.
+#include <algorithm>
 #include <cmath>
-#include <type_traits>
 #include <cstring>
 #include <new>
+#include <type_traits>
 #include <vector>
-#include <algorithm>
 
 #include "sl_device.h"
 #include "sl_internal.h"

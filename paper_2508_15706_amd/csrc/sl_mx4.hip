@@ -199,9 +199,10 @@ int slk_mx4_quantize(const void *src, int type, long long rows, long long cols, 
                      hipStream_t st)
 {
     QuantArgs A;
-    if (!sl_mx4_shape(rows, cols, A.s) || !sl_mx4_shape(cols, rows, A.t)) return SL_ERR_INVALID_ARG;
+    A.s = A.t = SlMx4Shape{};
+    if ((q && !sl_mx4_shape(rows, cols, A.s)) || (qt && !sl_mx4_shape(cols, rows, A.t))) return SL_ERR_INVALID_ARG;
     A.src = src, A.rows = rows, A.cols = cols, A.ld = ld, A.q = q, A.qt = qt;
-    A.col_groups = A.s.col_tiles;
+    A.col_groups = (cols + MX_COLS - 1) / MX_COLS;
     // qt's tiles are 128 of these rows deep and are filled up, also past the last row
     const long long row_groups = type == SL_TYPE_BF16 ? (rows + 127) / 128 : qt ? (rows + 127) / 128 * 2 : (rows + 63) / 64;
     const unsigned groups = (unsigned)(row_groups * A.col_groups);
@@ -220,11 +221,11 @@ size_t sl_mx4_bytes(int64_t rows, int64_t cols)
 
 int sl_mx4_quantize(const void *src, int src_type, int64_t rows, int64_t cols, int64_t ld, void *q, void *qt, void *stream)
 {
-    SlMx4Shape s, t;
+    SlMx4Shape s;
     if (rows < 0 || cols < 0) return SL_ERR_INVALID_ARG;
     if (rows == 0 || cols == 0) return SL_OK;
-    if (!src || (!q && !qt) || q == qt || q == src || qt == src || !sl_mx4_shape(rows, cols, s) || !sl_mx4_shape(cols, rows, t))
-        return SL_ERR_INVALID_ARG;
+    if (!src || (!q && !qt) || q == qt || q == src || qt == src) return SL_ERR_INVALID_ARG;
+    if ((q && !sl_mx4_shape(rows, cols, s)) || (qt && !sl_mx4_shape(cols, rows, s))) return SL_ERR_INVALID_ARG;
     if (src_type != SL_TYPE_F32 && src_type != SL_TYPE_BF16) return SL_ERR_INVALID_ARG;
     if (ld < cols || ld > ((int64_t)1 << 40) || misaligned(q, 16) || misaligned(qt, 16) || misaligned(src, src_type == SL_TYPE_BF16 ? 2 : 4))
         return SL_ERR_INVALID_ARG;

@@ -120,7 +120,7 @@ SL_DEV void stage_barrier()
 // this one's.
 // Row i of a result's tile is not b's row i: i = 8 g + 4 q + e takes 16 (g / 2) + 8 q + 4 (g % 2) + e, so that a lane has
 // eight consecutive columns of c twice.
-// PARTS: the contraction in parts, each of which writes its own fp32 c (slot blockIdx / tiles).
+// Workgroup `tiles` and on: the next part of the contraction, with a c of its own.
 template <bool B16, int TM, int TN, int STAGES, int WGS>
 __global__ void __launch_bounds__(256, WGS) k_product(ProductArgs A)
 {
