@@ -459,7 +459,8 @@ int sl_mx4_dequantize(const void *q, int64_t rows, int64_t cols, void *out, int 
  * c          device, m x n of c_type, row i at element i*ldc (ldc >= n), aligned to its element
  * accumulate only with SL_TYPE_F32
  * m, n >= 0, m*n <= 2^36; k >= 0 (k = 0: sums of nothing; a and b are not read)
- * workspace  device, sl_mx4_workspace_bytes(m, n, k), 16-byte aligned; may be NULL where that is 0 */
+ * workspace  device, sl_mx4_workspace_bytes(m, n, k), 16-byte aligned; may be NULL where that is 0.  The size
+ *            never falls as m, n or k grow: the workspace of the largest call serves every call whose m, n and k are no larger. */
 size_t sl_mx4_workspace_bytes(int64_t m, int64_t n, int64_t k);
 int sl_mx4_product(const void *a, const void *b, int64_t m, int64_t n, int64_t k, void *c, int c_type, int64_t ldc,
                    int accumulate, void *workspace, void *stream);

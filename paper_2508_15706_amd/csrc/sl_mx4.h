@@ -6,9 +6,7 @@
 // word per lane whose four bytes serve the four operands of 64 rows x 128 columns.
 #pragma once
 #include "sl_device.h"
-
-enum { MX_ROWS = 32, MX_COLS = 128, MX_BLOCK = 32, MX_TILE_BYTES = 2048, MX_SCALE_ROWS = 64, MX_SCALE_TILE_BYTES = 256,
-       MX_MOST_TILES = 1 << 22 };      // (a grid has less than 2^32 threads)
+#include "sl_mx4_rules.h"
 
 struct SlMx4Shape {
     long long rows, cols;

@@ -418,40 +418,6 @@ bool bad_sizes(int64_t m, int64_t n, int64_t k)
     return m > ((int64_t)1 << 36) / n || !sl_mx4_shape(m, k > 0 ? k : 1, s) || !sl_mx4_shape(n, k > 0 ? k : 1, s);
 }
 
-struct Choice {
-    int tile;                            // 0: 64 x 64, 1: 128 x 128, 2: 128 x 256
-    int parts;                           // of the contraction
-};
-
-// Tenths of a round (see below) that so many of the larger tiles take.
-int64_t rounds10(int64_t tiles) { return tiles / 512 * 10 + (tiles % 512 == 0 ? 0 : tiles % 512 <= 256 ? 6 : 10); }
-
-// By how many tiles there are for the 256 compute units (us, 64 x 64 / 128 x 128 / 128 x 256):
-//   few: every one gets a tile as soon as they are small - 1024 x 1024 x 4096 7.3 / 11.0 / 17.8, 256 x 8192 x 2048 7.0 / 7.8 / 11.6 -
-//   until 64 x 64 are more than two to a compute unit: 2388 x 956 x 16,370 (570) 46 / 34 / 58, 1024 x 4096 x 1024 8.8 / 6.8 / 9.1, 2048 cubed
-//   11.8 / 8.7 / 12.5;
-//   many: 512 workgroups of either larger tile run at a time, two to a compute unit, and a round of 128 x 256 takes 1.75 times as long as one of
-//   128 x 128 (it reads LDS less for the same products, and power is what bounds them); up to 256 tiles that are left over run one to a unit,
-//   in 0.6 of a round.  So the rounds decide: 8192 x 2048 x 16,384 (512 and 1024 tiles) - / 138 / 128, 8575 x 1866 x 3815 (536 and 1005) 72 / 41 / 48,
-//   517 x 50,257 x 2048 (985 and 1965) 72 / 46 / 40.5, 12,688 x 1510 x 323 (600 and 1200) 21.4 / 15.6 / 16.4, 5054 x 4236 x 5982 (680 and 1360)
-//   124 / 77 / 72.
-// A long contraction on very few tiles is cut into parts of 12 steps or more, whose results a second launch adds: 100 x 1000 x 16,384
-// (32 tiles, 128 steps) 19.4 whole, 9.9 in eight parts; 55 x 613 x 6252 (10 tiles, 49 steps) 8.9, 7.4 in four; 2378 x 67 x 11,212 (76 tiles)
-// 15.1, 11.8 in four; from 128 tiles on it gains nothing (256 x 2048 x 8192 11.4 and 11.6 in two).
-// (Over 60 sizes drawn from 16 .. 16,384 x 16 .. 8192 x 16 .. 16,384 the rule's choice takes 1 to 2 % longer than the best of the three sizes in
-// one, two, four or eight parts.)
-Choice choose(int64_t m, int64_t n, int64_t k)
-{
-    const int64_t small = ((m + 63) / 64) * ((n + 63) / 64), middle = ((m + 127) / 128) * ((n + 127) / 128),
-                  large = ((m + 127) / 128) * ((n + 255) / 256), steps = (k + MX_COLS - 1) / MX_COLS;
-    if (small > 512) return Choice{7 * rounds10(large) < 4 * rounds10(middle) ? 2 : 1, 1};
-    if (small > 100 || steps < 36) return Choice{0, 1};
-    const int64_t per = std::max<int64_t>({12, (steps + 7) / 8, (steps * small + 383) / 384});
-    return Choice{0, (int)((steps + per - 1) / per)};
-}
-
-long long part_pitch(int64_t n) { return (n + 3) / 4 * 4; }
-
 template <bool B16, int TM, int TN, int STAGES, int WGS>
 int launch_tiles(ProductArgs A, int parts, hipStream_t st)
 {
@@ -471,7 +437,7 @@ int launch_tiles(ProductArgs A, int parts, hipStream_t st)
 }
 
 template <bool B16>
-int launch(const ProductArgs &A, Choice c, hipStream_t st)
+int launch(const ProductArgs &A, SlMx4Choice c, hipStream_t st)
 {
     return c.tile == 0 ? launch_tiles<B16, 1, 1, 4, 4>(A, c.parts, st)
          : c.tile == 1 ? launch_tiles<B16, 2, 2, 4, 2>(A, c.parts, st)
@@ -488,7 +454,7 @@ int product(const unsigned char *a, const unsigned char *b, int64_t m, int64_t n
         (void)sl_mx4_shape(m, k, sa);
         (void)sl_mx4_shape(n, k, sb);
     }
-    const Choice how = choose(m, n, k);
+    const SlMx4Choice how = sl_mx4_choose(m, n, k);
     A.a = a, A.b = b;
     A.a_tiles = sa.row_tiles, A.b_tiles = sb.row_tiles, A.k_tiles = k > 0 ? sa.col_tiles : 0;
     A.a_scales = sa.scales, A.b_scales = sb.scales;
@@ -497,7 +463,7 @@ int product(const unsigned char *a, const unsigned char *b, int64_t m, int64_t n
     if (how.parts == 1)
         return type == SL_TYPE_BF16 ? launch<true>(A, how, st) : launch<false>(A, how, st);
     ProductArgs P = A;
-    const long long ldp = part_pitch(n);
+    const long long ldp = sl_mx4_part_pitch(n);
     P.c = parts, P.ldc = ldp, P.part_size = A.part_size = m * ldp, P.accumulate = 0;
     if (const int rc = launch<false>(P, how, st)) return rc;
     const dim3 grid((unsigned)((m * (ldp / 4) + 255) / 256));
@@ -507,10 +473,6 @@ int product(const unsigned char *a, const unsigned char *b, int64_t m, int64_t n
 
 // Bytes of LDS for the few rows' kernel: the sums of the waves and x in 4 bits.
 int64_t few_rows_lds(int64_t m, int64_t k) { return 8 * 1024 + (k + MX_COLS - 1) / MX_COLS * m * 68; }
-
-// Where it is not quicker to quantise x once, in a launch of its own: up to 640 steps of 128 in x's rows together (us, this kernel / two
-// launches: 8 rows, k = 8192 9.9 / 14.8, 16 rows, k = 2048 6.6 / 8.6, 16 rows, k = 8192 22.5 / 14.8).  That is at most 52 KB of LDS.
-bool few_rows(int64_t m, int64_t k) { return m <= 16 && m * ((k + MX_COLS - 1) / MX_COLS) <= 640; }
 
 template <bool X16, bool Y16>
 int launch_few_rows(const FewArgs &A, int64_t lds, hipStream_t st)
@@ -529,6 +491,9 @@ int launch_few_rows(const FewArgs &A, int64_t lds, hipStream_t st)
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
+// True where a call without a workspace is refused: more than few rows, or a contraction in parts.
+bool needs_room(int64_t m, int64_t n, int64_t k) { return k > 0 && (!sl_mx4_few_rows(m, k) || sl_mx4_choose(m, n, k).parts > 1); }
+
 }  // namespace
 
 extern "C" {
@@ -536,8 +501,7 @@ extern "C" {
 size_t sl_mx4_workspace_bytes(int64_t m, int64_t n, int64_t k)
 {
     if (bad_sizes(m, n, k) || m == 0 || n == 0 || k == 0) return 0;
-    const int parts = choose(m, n, k).parts;
-    return (few_rows(m, k) ? 0 : align256(sl_mx4_bytes(m, k))) + (parts > 1 ? parts * sizeof(float) * (size_t)(m * part_pitch(n)) : 0);
+    return (sl_mx4_few_rows(m, k) ? 0 : align256(sl_mx4_bytes(m, k))) + sizeof(float) * (size_t)sl_mx4_parts_room(m, n, k);
 }
 
 int sl_mx4_product(const void *a, const void *b, int64_t m, int64_t n, int64_t k, void *c, int c_type, int64_t ldc,
@@ -549,7 +513,7 @@ int sl_mx4_product(const void *a, const void *b, int64_t m, int64_t n, int64_t k
     if (!c || (k > 0 && (!a || !b)) || c == a || c == b || ldc < n || ldc > LONGEST) return SL_ERR_INVALID_ARG;
     if (misaligned(a, 16) || misaligned(b, 16) || misaligned(c, c_type == SL_TYPE_BF16 ? 2 : 4) || misaligned(workspace, 16))
         return SL_ERR_INVALID_ARG;
-    if (!workspace && sl_mx4_workspace_bytes(m, n, k)) return SL_ERR_INVALID_ARG;
+    if (!workspace && needs_room(m, n, k)) return SL_ERR_INVALID_ARG;
     return product(static_cast<const unsigned char *>(a), static_cast<const unsigned char *>(b), m, n, k, c, c_type, ldc,
                    accumulate, static_cast<float *>(workspace), static_cast<hipStream_t>(stream));
 }
@@ -564,9 +528,9 @@ int sl_mx4_linear(const void *x, int x_type, int64_t ldx, const void *w, int64_t
     if (misaligned(x, x_type == SL_TYPE_BF16 ? 2 : 4) || misaligned(w, 16) || misaligned(y, y_type == SL_TYPE_BF16 ? 2 : 4) ||
         misaligned(workspace, 16))
         return SL_ERR_INVALID_ARG;
-    if (!workspace && sl_mx4_workspace_bytes(m, n, k)) return SL_ERR_INVALID_ARG;
+    if (!workspace && needs_room(m, n, k)) return SL_ERR_INVALID_ARG;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (k > 0 && few_rows(m, k)) {
+    if (k > 0 && sl_mx4_few_rows(m, k)) {
         FewArgs A;
         A.x = x, A.ldx = ldx, A.w = static_cast<const unsigned char *>(w), A.m = (int)m, A.y = y, A.ldy = ldy;
         (void)sl_mx4_shape(n, k, A.s);

@@ -1,0 +1,27 @@
+"""Products of 4-bit matrices without a GPU: the rule that chooses their kernels, and the room that they ask for."""
+import os
+import subprocess
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+ROOT = os.path.dirname(HERE)
+
+
+def test_rules(tmp_path):
+    exe = str(tmp_path / "mx4_rules")
+    # (signed overflow ends the program instead of wrapping)
+    cmd = ["g++", "-std=c++17", "-O2", "-fsanitize=signed-integer-overflow", "-fsanitize-undefined-trap-on-error",
+           "-I", os.path.join(ROOT, "paper_2508_15706_amd", "csrc"), os.path.join(HERE, "host", "mx4_rules.cpp"), "-o", exe]
+    subprocess.run(cmd, check=True)
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert (r.returncode, r.stdout.strip()) == (0, "ok"), r.stdout + r.stderr
+
+
+@pytest.mark.parametrize("m, n, k", [(2000, 512, 8192), (512, 2048, 8192), (512, 1024, 8192), (70, 700, 16384), (16, 2048, 8192)])
+def test_room_for_the_most_rows_serves_fewer(m, n, k):
+    from paper_2508_15706_amd import binding as sl
+    most = sl.sl_mx4_workspace_bytes(m, n, k)
+    assert all(sl.sl_mx4_workspace_bytes(rows, n, k) <= most for rows in range(1, m))
+    assert all(sl.sl_mx4_workspace_bytes(m, cols, k) <= most for cols in range(1, n, 7))
+    assert all(sl.sl_mx4_workspace_bytes(m, n, length) <= most for length in range(1, k, 31))
