@@ -465,7 +465,8 @@ size_t sl_mx4_workspace_bytes(int64_t m, int64_t n, int64_t k);
 int sl_mx4_product(const void *a, const void *b, int64_t m, int64_t n, int64_t k, void *c, int c_type, int64_t ldc,
                    int accumulate, void *workspace, void *stream);
 /* y = Q(x) w^T for a dense x (m x k of x_type, row i at element i*ldx): sl_mx4_quantize of x and
- * sl_mx4_product in one call; for a few rows (generation, one token per sequence) in one launch. */
+ * sl_mx4_product in one call; for a few rows (generation, one token per sequence; m <= 16 and
+ * m * ceil(k / 128) <= 640) in one launch, which uses no workspace: NULL will do. */
 int sl_mx4_linear(const void *x, int x_type, int64_t ldx, const void *w, int64_t m, int64_t n, int64_t k, void *y,
                   int y_type, int64_t ldy, void *workspace, void *stream);
 

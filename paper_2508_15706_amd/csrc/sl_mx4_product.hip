@@ -491,9 +491,6 @@ int launch_few_rows(const FewArgs &A, int64_t lds, hipStream_t st)
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
-// True where a call without a workspace is refused: more than few rows, or a contraction in parts.
-bool needs_room(int64_t m, int64_t n, int64_t k) { return k > 0 && (!sl_mx4_few_rows(m, k) || sl_mx4_choose(m, n, k).parts > 1); }
-
 }  // namespace
 
 extern "C" {
@@ -513,7 +510,7 @@ int sl_mx4_product(const void *a, const void *b, int64_t m, int64_t n, int64_t k
     if (!c || (k > 0 && (!a || !b)) || c == a || c == b || ldc < n || ldc > LONGEST) return SL_ERR_INVALID_ARG;
     if (misaligned(a, 16) || misaligned(b, 16) || misaligned(c, c_type == SL_TYPE_BF16 ? 2 : 4) || misaligned(workspace, 16))
         return SL_ERR_INVALID_ARG;
-    if (!workspace && needs_room(m, n, k)) return SL_ERR_INVALID_ARG;
+    if (!workspace && k > 0 && (!sl_mx4_few_rows(m, k) || sl_mx4_choose(m, n, k).parts > 1)) return SL_ERR_INVALID_ARG;
     return product(static_cast<const unsigned char *>(a), static_cast<const unsigned char *>(b), m, n, k, c, c_type, ldc,
                    accumulate, static_cast<float *>(workspace), static_cast<hipStream_t>(stream));
 }
@@ -528,7 +525,6 @@ int sl_mx4_linear(const void *x, int x_type, int64_t ldx, const void *w, int64_t
     if (misaligned(x, x_type == SL_TYPE_BF16 ? 2 : 4) || misaligned(w, 16) || misaligned(y, y_type == SL_TYPE_BF16 ? 2 : 4) ||
         misaligned(workspace, 16))
         return SL_ERR_INVALID_ARG;
-    if (!workspace && needs_room(m, n, k)) return SL_ERR_INVALID_ARG;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (k > 0 && sl_mx4_few_rows(m, k)) {
         FewArgs A;
@@ -538,6 +534,7 @@ int sl_mx4_linear(const void *x, int x_type, int64_t ldx, const void *w, int64_t
         if (x_type == SL_TYPE_BF16) return y_type == SL_TYPE_BF16 ? launch_few_rows<true, true>(A, lds, st) : launch_few_rows<true, false>(A, lds, st);
         return y_type == SL_TYPE_BF16 ? launch_few_rows<false, true>(A, lds, st) : launch_few_rows<false, false>(A, lds, st);
     }
+    if (!workspace && k > 0) return SL_ERR_INVALID_ARG;
     unsigned char *q = static_cast<unsigned char *>(workspace);
     if (k > 0)
         if (const int rc = slk_mx4_quantize(x, x_type, m, k, ldx, q, nullptr, st)) return rc;
