@@ -402,7 +402,8 @@ typedef struct {
  * grad         in, device, arena of grad_type, 16-byte aligned
  * grad_scale   in, device, one float, or NULL; if it is NaN nothing is written at all
  * theta16      out, device, or NULL: a bf16 arena that receives theta rounded to nearest
- * 0 <= beta1, beta2 < 1, eps > 0, step >= 1, all finite, else INVALID_ARG. */
+ * 0 <= beta1, beta2 < 1, eps > 0, step >= 1, all finite, and so are eps and the constants above in
+ * fp32 (an eps below its smallest number is 0 there), else INVALID_ARG. */
 int sl_adamw_step(sl_adamw *opt, float *theta, const void *grad, int grad_type, float *m, float *v,
                   const sl_adamw_params *params, const float *grad_scale, void *theta16, void *stream);
 

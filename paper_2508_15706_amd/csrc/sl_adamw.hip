@@ -390,7 +390,8 @@ int check_device(const sl_adamw *o)
 
 bool bad_type(int t) { return t != SL_TYPE_F32 && t != SL_TYPE_BF16; }
 
-// The constants of a step; false where a parameter is out of range.
+// The constants of a step; false where a parameter is out of range, or a constant in fp32: an eps that is 0 there divides 0 by 0
+// wherever a gradient has always been zero, an infinite factor makes NaN of the zeros it meets.
 bool step_constants(const sl_adamw_params *P, StepArgs &A)
 {
     if (!P || P->step < 1) return false;
@@ -402,7 +403,7 @@ bool step_constants(const sl_adamw_params *P, StepArgs &A)
     A.r = (float)(1.0 / std::sqrt(1.0 - std::pow(P->beta2, (double)P->step)));
     A.eps = (float)P->eps;
     A.shrink = (float)(P->lr * P->weight_decay);
-    return true;
+    return A.eps > 0.0f && std::isfinite(A.eps) && std::isfinite(A.rate) && std::isfinite(A.r) && std::isfinite(A.shrink);
 }
 
 unsigned host_fmix(unsigned h)
