@@ -525,15 +525,20 @@ def _mx4_ptr(q: Optional[torch.Tensor], rows: int, cols: int) -> Optional[int]:
     return _dev_ptr(q, torch.uint8)
 
 
+def _room(what: str, t: Optional[torch.Tensor], size: int, dtype=None) -> Optional[int]:
+    """Pointer of a contiguous device tensor of at least `size` elements."""
+    if t is not None and t.numel() < size:
+        raise ValueError(f"{what} has {t.numel()} elements, {size} are needed")
+    return _dev_ptr(t, dtype)
+
+
 class AdamW:
-    """Owner of an sl_adamw handle."""
+    """Owner of an sl_adamw handle, and what its calls need: elements of an arena up to the end of its last tensor, blocks of
+    the 8-bit states, bytes of the norm's workspace."""
 
-    def __init__(self, handle: int, n_tensors: int):
+    def __init__(self, handle: Optional[int], n_tensors: int, arena: int, num_blocks: int, norm_bytes: int):
         self.handle, self.n_tensors = handle, n_tensors
-
-    @property
-    def num_blocks(self) -> int:
-        return int(lib().sl_adamw_num_blocks(self.handle))
+        self.arena, self.num_blocks, self.norm_bytes = arena, num_blocks, norm_bytes
 
     def close(self):
         if self.handle:
@@ -560,18 +565,20 @@ def sl_adamw_create(descs: Sequence[Sequence[int]], decay: Optional[Sequence[flo
     st = lib().sl_adamw_create(arr, len(descs), factors, C.byref(h))
     if st:
         raise SparseLoCoError("sl_adamw_create", st)
-    return AdamW(h.value, len(descs))
+    return AdamW(h.value, len(descs), max((int(r) * int(c) + int(off) for r, c, off, _ in descs), default=0),
+                 int(lib().sl_adamw_num_blocks(h.value)), int(lib().sl_grad_norm_workspace_bytes(h.value)))
 
 
 def alloc_norm_workspace(opt: AdamW, device="cuda") -> torch.Tensor:
-    return torch.empty(int(lib().sl_grad_norm_workspace_bytes(opt.handle)), dtype=torch.uint8, device=device)
+    return torch.empty(opt.norm_bytes, dtype=torch.uint8, device=device)
 
 
 def sl_grad_norm(opt: AdamW, grad: torch.Tensor, max_norm: float, result: torch.Tensor, workspace: torch.Tensor,
                  stream=None) -> None:
     """result: two fp32 values, the norm and the factor that clips it (grad_scale of a step: result[1:])."""
-    st = lib().sl_grad_norm(opt.handle, _dev_ptr(grad), _type_of(grad), float(max_norm),
-                            _dev_ptr(result, torch.float32), _dev_ptr(workspace, torch.uint8), _stream_ptr(stream))
+    st = lib().sl_grad_norm(opt.handle, _room("grad", grad, opt.arena), _type_of(grad), float(max_norm),
+                            _room("result", result, 2, torch.float32),
+                            _room("workspace", workspace, opt.norm_bytes, torch.uint8), _stream_ptr(stream))
     if st:
         raise SparseLoCoError("sl_grad_norm", st)
 
@@ -579,10 +586,11 @@ def sl_grad_norm(opt: AdamW, grad: torch.Tensor, max_norm: float, result: torch.
 def sl_adamw_step(opt: AdamW, theta: torch.Tensor, grad: torch.Tensor, m: torch.Tensor, v: torch.Tensor, lr: float,
                   beta1: float, beta2: float, eps: float, weight_decay: float, step: int,
                   grad_scale: Optional[torch.Tensor] = None, theta16: Optional[torch.Tensor] = None, stream=None) -> None:
-    params = SlAdamwParams(lr, beta1, beta2, eps, weight_decay, step)
-    st = lib().sl_adamw_step(opt.handle, _dev_ptr(theta, torch.float32), _dev_ptr(grad), _type_of(grad),
-                             _dev_ptr(m, torch.float32), _dev_ptr(v, torch.float32), C.byref(params),
-                             _dev_ptr(grad_scale, torch.float32), _dev_ptr(theta16, torch.bfloat16), _stream_ptr(stream))
+    params, n = SlAdamwParams(lr, beta1, beta2, eps, weight_decay, step), opt.arena
+    st = lib().sl_adamw_step(opt.handle, _room("theta", theta, n, torch.float32), _room("grad", grad, n), _type_of(grad),
+                             _room("m", m, n, torch.float32), _room("v", v, n, torch.float32), C.byref(params),
+                             _room("grad_scale", grad_scale, 1, torch.float32), _room("theta16", theta16, n, torch.bfloat16),
+                             _stream_ptr(stream))
     if st:
         raise SparseLoCoError("sl_adamw_step", st)
 
@@ -591,20 +599,21 @@ def sl_adamw_step8(opt: AdamW, theta: torch.Tensor, grad: torch.Tensor, m_codes:
                    m_scales: torch.Tensor, v_scales: torch.Tensor, seed: int, lr: float, beta1: float, beta2: float,
                    eps: float, weight_decay: float, step: int, grad_scale: Optional[torch.Tensor] = None,
                    theta16: Optional[torch.Tensor] = None, stream=None) -> None:
-    params = SlAdamwParams(lr, beta1, beta2, eps, weight_decay, step)
-    st = lib().sl_adamw_step8(opt.handle, _dev_ptr(theta, torch.float32), _dev_ptr(grad), _type_of(grad),
-                              _dev_ptr(m_codes, torch.uint8), _dev_ptr(v_codes, torch.uint8),
-                              _dev_ptr(m_scales, torch.uint8), _dev_ptr(v_scales, torch.uint8), int(seed) & 0xFFFFFFFF,
-                              C.byref(params), _dev_ptr(grad_scale, torch.float32), _dev_ptr(theta16, torch.bfloat16),
-                              _stream_ptr(stream))
+    params, n, blocks = SlAdamwParams(lr, beta1, beta2, eps, weight_decay, step), opt.arena, opt.num_blocks
+    st = lib().sl_adamw_step8(opt.handle, _room("theta", theta, n, torch.float32), _room("grad", grad, n), _type_of(grad),
+                              _room("m_codes", m_codes, n, torch.uint8), _room("v_codes", v_codes, n, torch.uint8),
+                              _room("m_scales", m_scales, blocks, torch.uint8), _room("v_scales", v_scales, blocks, torch.uint8),
+                              int(seed) & 0xFFFFFFFF, C.byref(params), _room("grad_scale", grad_scale, 1, torch.float32),
+                              _room("theta16", theta16, n, torch.bfloat16), _stream_ptr(stream))
     if st:
         raise SparseLoCoError("sl_adamw_step8", st)
 
 
 def sl_adamw_state_values(opt: AdamW, moment: int, codes: torch.Tensor, scales: torch.Tensor, values: torch.Tensor,
                           stream=None) -> None:
-    st = lib().sl_adamw_state_values(opt.handle, int(moment), _dev_ptr(codes, torch.uint8), _dev_ptr(scales, torch.uint8),
-                                     _dev_ptr(values, torch.float32), _stream_ptr(stream))
+    st = lib().sl_adamw_state_values(opt.handle, int(moment), _room("codes", codes, opt.arena, torch.uint8),
+                                     _room("scales", scales, opt.num_blocks, torch.uint8),
+                                     _room("values", values, opt.arena, torch.float32), _stream_ptr(stream))
     if st:
         raise SparseLoCoError("sl_adamw_state_values", st)
 
