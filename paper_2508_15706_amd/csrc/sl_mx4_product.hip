@@ -101,11 +101,15 @@ SL_DEV TilePlace tile_place(unsigned i, unsigned tiles, long long m_tiles, long 
 
 // 16 (scales: the same) bytes per lane from memory to LDS at `lds` + 16 * lane, past the registers.  The instruction is
 // written out because the compiler, which cannot tell the stages apart, would wait for all of them before every read
-// of LDS; it has no result in a register, the waits for it are written out too, and nothing else in these kernels uses m0.
+// of LDS; it has no result in a register, and the waits for it are written out too.  (m0 is the compiler's own, which warns that it will not
+// be kept: that is what the list of clobbers is to say.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 SL_DEV void dma16(const unsigned char *base, unsigned lane_off, unsigned lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(lane_off), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(lane_off), "s"(base) : "m0", "memory");
 }
+#pragma clang diagnostic pop
 template <int N>
 SL_DEV void wait_dma() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 // All waves' reads of LDS are done and have arrived.
