@@ -484,10 +484,7 @@ int launch_few_rows(const FewArgs &A, int64_t lds, hipStream_t st)
     typedef void (*kernel_t)(FewArgs);
     static const kernel_t table[4] = {k_few_rows<X16, Y16, 1>, k_few_rows<X16, Y16, 2>, k_few_rows<X16, Y16, 4>, k_few_rows<X16, Y16, 8>};
     const int64_t tiles = (A.s.rows + 15) / 16;
-    // waves per tile: about 2048 of them in all (k = 2048, 512 tiles, 1 / 2 / 4 / 8 waves: 4.5 / 3.8 / 3.5 / 4.2; k = 8192, 128 tiles: 10.1 / 6.8 /
-    // 5.2 / 4.4; k = 2048, 3142 tiles: 11.1 / 12.0 / 14.1 / 17.8)
-    int log2 = 0;
-    while (log2 < 3 && (tiles << log2) < 2048) ++log2;
+    const int log2 = sl_mx4_few_waves_log2(A.s.rows);
     const int64_t per = 8 >> log2;
     hipLaunchKernelGGL(table[log2], dim3((unsigned)((tiles + per - 1) / per)), dim3(512), (unsigned)lds, st, A);
     return check_launch();

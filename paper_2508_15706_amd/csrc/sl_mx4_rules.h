@@ -63,3 +63,12 @@ inline int64_t sl_mx4_parts_room(int64_t m, int64_t n, int64_t k)
 // Where it is not quicker to quantise x once, in a launch of its own: up to 640 steps of 128 in x's rows together (us, this kernel / two
 // launches: 8 rows, k = 8192 9.9 / 14.8, 16 rows, k = 2048 6.6 / 8.6, 16 rows, k = 8192 22.5 / 14.8).  That is at most 52 KB of LDS.
 inline bool sl_mx4_few_rows(int64_t m, int64_t k) { return m <= 16 && m * ((k + MX_COLS - 1) / MX_COLS) <= 640; }
+
+// Waves that share a tile of 16 columns of the few rows' result, as a power of two: about 2048 waves in all (us, 1 / 2 / 4 / 8 waves to a tile, k = 2048,
+// 512 tiles: 4.5 / 3.8 / 3.5 / 4.2; k = 8192, 128 tiles: 10.1 / 6.8 / 5.2 / 4.4; k = 2048, 3142 tiles: 11.1 / 12.0 / 14.1 / 17.8).
+inline int sl_mx4_few_waves_log2(int64_t n)
+{
+    int log2 = 0;
+    while (log2 < 3 && ((n + 15) / 16 << log2) < 2048) ++log2;
+    return log2;
+}

@@ -1,6 +1,7 @@
-// Products of 4-bit matrices: the room for the parts of a contraction serves every smaller product, and every size of kernel is chosen
-// for the sizes that the GPU tests reach it with.
+// Products of 4-bit matrices: the room for the parts of a contraction serves every smaller product.  With arguments, m n k of any number of products,
+// prints which kernel serves each: its tile, the parts of the contraction, whether there are few rows, and the waves to a tile for those.
 #include <cstdio>
+#include <cstdlib>
 
 #include "sl_mx4_rules.h"
 
@@ -39,8 +40,14 @@ static void room()
             if (needed(64 * tiles, 64, 128 * steps) > sl_mx4_parts_room(64 * tiles, 64, 128 * steps)) fail("its own parts", 64 * tiles, 64, 128 * steps);
 }
 
-int main()
+int main(int argc, char **argv)
 {
+    for (int i = 1; i + 2 < argc; i += 3) {
+        const long long m = std::atoll(argv[i]), n = std::atoll(argv[i + 1]), k = std::atoll(argv[i + 2]);
+        const SlMx4Choice c = sl_mx4_choose(m, n, k);
+        std::printf("%d %d %d %d\n", c.tile, c.parts, (int)sl_mx4_few_rows(m, k), 1 << sl_mx4_few_waves_log2(n));
+    }
+    if (argc > 1) return 0;
     room();
     if (!failures) std::printf("ok\n");
     return failures ? 1 : 0;
