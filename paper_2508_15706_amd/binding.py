@@ -502,9 +502,10 @@ _TYPES = {torch.float32: 0, torch.bfloat16: 1}            # SL_TYPE_F32, SL_TYPE
 
 
 def _type_of(t: torch.Tensor) -> int:
-    if t.dtype not in _TYPES:
+    typ = _TYPES.get(t.dtype)
+    if typ is None:
         raise ValueError(f"expected float32 or bfloat16, got {t.dtype}")
-    return _TYPES[t.dtype]
+    return typ
 
 
 def _matrix(t: torch.Tensor):
@@ -525,11 +526,17 @@ def _mx4_ptr(q: Optional[torch.Tensor], rows: int, cols: int) -> Optional[int]:
     return _dev_ptr(q, torch.uint8)
 
 
-def _room(what: str, t: Optional[torch.Tensor], size: int, dtype=None) -> Optional[int]:
-    """Pointer of a contiguous device tensor of at least `size` elements."""
-    if t is not None and t.numel() < size:
+def _room(what: str, t: Optional[torch.Tensor], size: int, dtype: Optional[torch.dtype] = None) -> Optional[int]:
+    """_dev_ptr of a tensor of at least `size` elements (written out: a step has up to nine of them)."""
+    if t is None:
+        return None
+    if t.numel() < size:
         raise ValueError(f"{what} has {t.numel()} elements, {size} are needed")
-    return _dev_ptr(t, dtype)
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("expected a contiguous device tensor")
+    if dtype is not None and t.dtype is not dtype:
+        raise ValueError(f"expected dtype {dtype}, got {t.dtype}")
+    return t.data_ptr()
 
 
 class AdamW:
