@@ -379,8 +379,9 @@ size_t sl_grad_norm_workspace_bytes(const sl_adamw *opt);
 
 /* Norm of all gradients of the list and the factor that clips it:
  *   result[0] = sqrt(sum over all elements of grad^2)      (fp64 sums in a fixed order)
- *   result[1] = max_norm / norm where norm > max_norm, else 1; NaN where the norm is infinite
- *               or NaN.  A step that is given result + 1 as its grad_scale then clips, and
+ *   result[1] = max_norm / norm where norm > max_norm, else 1; NaN where a gradient is infinite
+ *               or NaN (a finite norm beyond fp32's range has a factor, and result[0] is
+ *               infinite).  A step that is given result + 1 as its grad_scale then clips, and
  *               leaves everything as it is where a gradient was not finite.
  * grad      in,  device, arena of grad_type, 16-byte aligned
  * max_norm  > 0 (infinity: no clipping)

@@ -35,3 +35,16 @@ def test_a_gradient_that_has_always_been_zero_leaves_theta_finite(change):
     codes = [torch.zeros(16, dtype=torch.uint8, device="cuda") for _ in range(4)]
     sl.sl_adamw_step8(opt, theta, grad, *codes, 1, **dict(PARAMS, **change))
     assert bool((theta == 1.0).all())
+
+
+def test_a_norm_beyond_fp32_still_clips():
+    """Finite gradients whose norm only fp64 holds: 3e38 * sqrt(8) = 8.5e38.  The factor is a subnormal, to within half of 2^-149."""
+    import torch
+    from paper_2508_15706_amd import binding as sl
+    opt = sl.sl_adamw_create([(1, 8, 0, 0)])
+    grad, out = torch.full((8,), 3e38, device="cuda"), torch.empty(2, device="cuda")
+    norm = float(grad[0]) * 8 ** 0.5
+    sl.sl_grad_norm(opt, grad, 1.0, out, sl.alloc_norm_workspace(opt))
+    assert out[0] == float("inf") and abs(float(out[1]) - 1 / norm) <= 2.0 ** -150 * (1 + 2.0 ** -20)
+    sl.sl_grad_norm(opt, grad, float("inf"), out, sl.alloc_norm_workspace(opt))
+    assert out.tolist() == [float("inf"), 1.0]
