@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(256) k_quantize(QuantArgs A)
 }
 
 // Eight elements - a word of codes - in a lane, 512 columns of a row in a wave, 16 rows in a workgroup: rows are written in pieces
-// of 1 KB (in pieces of 256 bytes, neighbours meet in the lines at the ends of unaligned ones: 2048 x 50,257 bf16 89 us, so 63).
+// of 1 KB (in pieces of 256 bytes, neighbours meet in the lines at the ends of unaligned ones: 2048 x 50,257 bf16 89 us, so 45).
 // HINT: streaming stores, for rows that begin on 16 bytes (50,257 x 2048 53 us without, 38 with).
 template <bool B16, bool HINT>
 __global__ void __launch_bounds__(256) k_dequantize(const unsigned char *q, SlMx4Shape s, void *out, long long ld, long long col_groups)

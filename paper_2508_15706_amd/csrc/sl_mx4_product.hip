@@ -316,8 +316,8 @@ __global__ void __launch_bounds__(256) k_join(ProductArgs A, const float *parts,
 // ---- few rows ----
 
 // y = Q(x) w^T for up to 16 rows of x, in the 16 x 16 x 128 shape of the matrix unit: lane l has block l / 16 of row
-// l % 16.  Every workgroup quantises x for itself, into LDS, while the first of w's bytes are on their way; its eight
-// waves then take 8 / KW tiles of 16 rows of w, KW waves for a tile, each every KW-th step of 128 of the contraction,
+// l % 16.  Every workgroup quantises x for itself, into LDS; w's first bytes are requested before x's, and loads complete in
+// the order of their requests, so that x is waited for together with them.  Its eight waves then take 8 / KW tiles of 16 rows of w, KW waves for a tile, each every KW-th step of 128 of the contraction,
 // and the sums of a tile's waves are added in their order.  Bound by the way of w's bytes to the registers, each of which is
 // used once, and for small layers by the launch.
 struct FewArgs {

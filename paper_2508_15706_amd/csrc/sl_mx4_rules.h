@@ -26,9 +26,10 @@ inline int64_t sl_mx4_rounds10(int64_t tiles) { return tiles / 512 * 10 + (tiles
 //   in 0.6 of a round.  So the rounds decide: 8192 x 2048 x 16,384 (512 and 1024 tiles) - / 138 / 128, 8575 x 1866 x 3815 (536 and 1005) 72 / 41 / 48,
 //   517 x 50,257 x 2048 (985 and 1965) 72 / 46 / 40.5, 12,688 x 1510 x 323 (600 and 1200) 21.4 / 15.6 / 16.4, 5054 x 4236 x 5982 (680 and 1360)
 //   124 / 77 / 72.
-// A long contraction on very few tiles is cut into parts of 12 steps or more, whose results a second launch adds: 100 x 1000 x 16,384
-// (32 tiles, 128 steps) 19.4 whole, 9.9 in eight parts; 55 x 613 x 6252 (10 tiles, 49 steps) 8.9, 7.4 in four; 2378 x 67 x 11,212 (76 tiles)
-// 15.1, 11.8 in four; from 128 tiles on it gains nothing (256 x 2048 x 8192 11.4 and 11.6 in two).
+// A long contraction on very few tiles is cut: parts of 12 steps, of more where there would be more than eight or than 384 workgroups; the steps are
+// then shared out evenly, and a second launch adds the parts' results.  In a graph, whole / four / five / eight parts: 100 x 1000 x 16,384 (32 tiles, 128 steps; the rule makes
+// eight) 19.1 / 10.3 / 10.0 / 10.2; 55 x 613 x 6252 (10 tiles, 49 steps; five) 8.7 / 7.1 / 7.2 / 7.7; 2378 x 67 x 11,212 (76 tiles, 88 steps; five)
+// 14.6 / 11.9 / 11.6 / 13.5; from 128 tiles on it gains nothing (256 x 2048 x 8192 11.0 / 13.9 / 16.0 / 19.0, two parts 11.4 and 11.6).
 // (Over 60 sizes drawn from 16 .. 16,384 x 16 .. 8192 x 16 .. 16,384 the rule's choice takes 1 to 2 % longer than the best of the three sizes in
 // one, two, four or eight parts.)
 inline SlMx4Choice sl_mx4_choose(int64_t m, int64_t n, int64_t k)
