@@ -527,16 +527,14 @@ def _mx4_ptr(q: Optional[torch.Tensor], rows: int, cols: int) -> Optional[int]:
 
 
 def _room(what: str, t: Optional[torch.Tensor], size: int, dtype: Optional[torch.dtype] = None) -> Optional[int]:
-    """_dev_ptr of a tensor of at least `size` elements (written out: a step has up to nine of them)."""
+    """_dev_ptr of a tensor of at least `size` elements.  (A step has up to nine of them: one condition, sorted out where it does not hold.)"""
     if t is None:
         return None
+    if t.numel() >= size and t.is_cuda and (dtype is None or t.dtype is dtype) and t.is_contiguous():
+        return t.data_ptr()
     if t.numel() < size:
         raise ValueError(f"{what} has {t.numel()} elements, {size} are needed")
-    if not t.is_cuda or not t.is_contiguous():
-        raise ValueError("expected a contiguous device tensor")
-    if dtype is not None and t.dtype is not dtype:
-        raise ValueError(f"expected dtype {dtype}, got {t.dtype}")
-    return t.data_ptr()
+    return _dev_ptr(t, dtype)
 
 
 class AdamW:
