@@ -451,7 +451,8 @@ size_t sl_mx4_bytes(int64_t rows, int64_t cols);
  * A matrix without rows or columns (an empty batch) is nothing to do. */
 int sl_mx4_quantize(const void *src, int src_type, int64_t rows, int64_t cols, int64_t ld, void *q, void *qt,
                     void *stream);
-/* The values of q, each rounded once where the type is bf16 and its exponent is out of range. */
+/* The values of q, each rounded once where its exponent is out of the type's range: bf16's and fp32's at the low
+ * end, and from X = 253 on 4 and 6 are infinite in either (4 * 2^126 = 2^128). */
 int sl_mx4_dequantize(const void *q, int64_t rows, int64_t cols, void *out, int out_type, int64_t ld, void *stream);
 
 /* c[i][j] = sum over l of a[i][l] * b[j][l]  (+ c[i][j] where accumulate is not 0), a of m x k, b of n x k:
