@@ -157,7 +157,7 @@ def prepare(case, seed):
             s["ws"] = sl.alloc_token_loss_workspace(rows)
         elif kind == "attend_step":
             s["ws"] = sl.alloc_attention_workspace(rows_q, q_heads)
-        elif token:
+        elif kind == "token":
             s["ws"] = sl.alloc_attention_token_workspace(n, rows_k, q_heads, kv_heads, dim)
     return s
 
