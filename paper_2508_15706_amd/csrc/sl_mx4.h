@@ -149,6 +149,26 @@ SL_DEV unsigned sl_quad_max(unsigned v)
     return max(v, (unsigned)sl_dpp<SL_DPP_XOR2>((int)v));
 }
 
+// Blocks of two columns: e[i] holds row i's elements of both in bf16; w their codes, x their scale bytes.
+SL_DEV void sl_mx4_columns(const unsigned (&e)[32], sl_u4 (&w)[2], unsigned (&x)[2])
+{
+    unsigned t = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) t = sl_pair_max(t, e[i] & 0x7FFF7FFFu);
+    x[0] = sl_mx4_scale(t << 16), x[1] = sl_mx4_scale(t & 0xFFFF0000u);
+    const float f0 = sl_mx4_factor(x[0]), f1 = sl_mx4_factor(x[1]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        unsigned o0 = 0, o1 = 0;
+#define SL_PAIR(J)                                                                       \
+    o0 = sl_mx4_pair<J>(o0, __builtin_amdgcn_perm(e[8 * i + 2 * J + 1], e[8 * i + 2 * J], 0x05040100u), f0); \
+    o1 = sl_mx4_pair<J>(o1, __builtin_amdgcn_perm(e[8 * i + 2 * J + 1], e[8 * i + 2 * J], 0x07060302u), f1);
+        SL_PAIR(0) SL_PAIR(1) SL_PAIR(2) SL_PAIR(3)
+#undef SL_PAIR
+        w[0][i] = x[0] == 255u ? 0u : o0, w[1][i] = x[1] == 255u ? 0u : o1;
+    }
+}
+
 // fp32 to bf16, to nearest, ties to even (the conversion instruction of this target).
 SL_DEV unsigned sl_bf16_bits(float x) { return (unsigned)__builtin_bit_cast(unsigned short, (__bf16)x); }
 SL_DEV unsigned sl_bf16_pair(float a, float b)

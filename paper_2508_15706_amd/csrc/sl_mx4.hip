@@ -79,27 +79,13 @@ __global__ void __launch_bounds__(256) k_quantize(QuantArgs A)
                 A.qt[A.t.scales + (ct / 2 * A.t.col_tiles + kt2) * MX_SCALE_TILE_BYTES + sl_mx4_scale_at(c, b)] = (unsigned char)x;
         };
         if constexpr (B16) {
-            unsigned e[32], t = 0;
+            unsigned e[32], x[2];
+            sl_u4 w[2];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                e[i] = words[(wave * 32 + i) * 64 + lane];
-                t = sl_pair_max(t, e[i] & 0x7FFF7FFFu);
-            }
-            const unsigned x0 = sl_mx4_scale(t << 16), x1 = sl_mx4_scale(t & 0xFFFF0000u);
-            const float f0 = sl_mx4_factor(x0), f1 = sl_mx4_factor(x1);
-            sl_u4 w0, w1;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                unsigned o0 = 0, o1 = 0;
-#define SL_PAIR(J)                                                                       \
-    o0 = sl_mx4_pair<J>(o0, __builtin_amdgcn_perm(e[8 * i + 2 * J + 1], e[8 * i + 2 * J], 0x05040100u), f0); \
-    o1 = sl_mx4_pair<J>(o1, __builtin_amdgcn_perm(e[8 * i + 2 * J + 1], e[8 * i + 2 * J], 0x07060302u), f1);
-                SL_PAIR(0) SL_PAIR(1) SL_PAIR(2) SL_PAIR(3)
-#undef SL_PAIR
-                w0[i] = x0 == 255u ? 0u : o0, w1[i] = x1 == 255u ? 0u : o1;
-            }
-            put(lane * 2, w0, x0);
-            put(lane * 2 + 1, w1, x1);
+            for (int i = 0; i < 32; ++i) e[i] = words[(wave * 32 + i) * 64 + lane];
+            sl_mx4_columns(e, w, x);
+            put(lane * 2, w[0], x[0]);
+            put(lane * 2 + 1, w[1], x[1]);
         } else {
             const int c = (wave & 1) * 64 + lane;
             SlOctet<false> e[4];

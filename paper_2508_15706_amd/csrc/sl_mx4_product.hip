@@ -2,6 +2,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "sl_dma.h"
 #include "sl_internal.h"
 #include "sl_mx4.h"
 
@@ -97,25 +98,6 @@ SL_DEV TilePlace tile_place(unsigned i, unsigned tiles, long long m_tiles, long 
     const unsigned band_size = 8u * (unsigned)n_tiles, band = at / band_size, in = at % band_size;
     const unsigned rows = min(8u, (unsigned)m_tiles - band * 8u);
     return TilePlace{(long long)(band * 8u + in % rows), (long long)(in / rows)};
-}
-
-// 16 (scales: the same) bytes per lane from memory to LDS at `lds` + 16 * lane, past the registers.  The instruction is
-// written out because the compiler, which cannot tell the stages apart, would wait for all of them before every read
-// of LDS; it has no result in a register, and the waits for it are written out too.  (m0 is the compiler's own, which warns that it will not
-// be kept: that is what the list of clobbers is to say.)
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-SL_DEV void dma16(const unsigned char *base, unsigned lane_off, unsigned lds)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(lane_off), "s"(base) : "m0", "memory");
-}
-#pragma clang diagnostic pop
-template <int N>
-SL_DEV void wait_dma() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
-// All waves' reads of LDS are done and have arrived.
-SL_DEV void stage_barrier()
-{
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
 // Four waves, 2 x 2, TM x TN tiles of 32 x 32 each: 64 TM x 64 TN of c in a workgroup.  Per step of 128 of the
