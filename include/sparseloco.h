@@ -473,6 +473,97 @@ int sl_mx4_product(const void *a, const void *b, int64_t m, int64_t n, int64_t k
 int sl_mx4_linear(const void *x, int x_type, int64_t ldx, const void *w, int64_t m, int64_t n, int64_t k, void *y,
                   int y_type, int64_t ldy, void *workspace, void *stream);
 
+/* ---- Root-mean-square norm of rows.
+ *
+ * h = x + residual, rounded to h_type (h = x where residual and h are NULL: both or neither)
+ * s = 1 / sqrt(mean of the row's h^2 + eps): summed in fp64, rounded to fp32
+ * y = (h s) weight, each product rounded to fp32, the last one to y_type
+ * x, residual, h, y   device, rows x cols, row i at element i*ld.., ld.. >= cols, aligned to their elements; residual has h_type
+ *                     and may be h itself (with ldr = ldh); no other two are the same
+ * weight    in, device, cols elements of w_type
+ * eps       1e-30 or more
+ * y, rstd, q, qt   out, each may be NULL: the result; s of every row (float[rows], for the backward pass); sl_mx4_quantize(y in bf16,
+ *                  q, qt), byte for byte, without y's way through memory
+ * rows <= 2^21, cols <= 2^20; no rows or columns: nothing to do. */
+int sl_rms_norm(const void *x, int x_type, int64_t ldx, const void *residual, int64_t ldr, void *h, int h_type, int64_t ldh,
+                const void *weight, int w_type, int64_t rows, int64_t cols, double eps, void *y, int y_type, int64_t ldy, float *rstd,
+                void *q, void *qt, void *stream);
+/* Its gradients: with g = dy weight and u = h s,
+ *   dx = dh + s (g - u mean of the row's g u)      (the gradient of x and of residual alike)
+ *   dweight = sum over the rows of dy u (+ dweight where accumulate is not 0)
+ * h, rstd   in, as sl_rms_norm was given or left them (h = x where there is no residual)
+ * dy        in, device, rows x cols of dy_type;  dh: in, of dx_type, the gradient that reaches h past the norm, or NULL
+ * dx        out, may be dh itself (with lddx = lddh), no other operand
+ * dweight   out, fp32, or NULL; then workspace may be NULL too
+ * workspace device, sl_rms_norm_workspace_bytes(rows, cols), 16-byte aligned; that of the largest call serves smaller ones.
+ * Without rows dweight is zero (as it was, where accumulate is not 0). */
+size_t sl_rms_norm_workspace_bytes(int64_t rows, int64_t cols);
+int sl_rms_norm_backward(const void *h, int h_type, int64_t ldh, const void *weight, int w_type, const float *rstd, const void *dy,
+                         int dy_type, int64_t lddy, const void *dh, int64_t lddh, void *dx, int dx_type, int64_t lddx, float *dweight,
+                         int accumulate, int64_t rows, int64_t cols, void *workspace, void *stream);
+
+/* ---- Loss of tokens from their logits, and its gradient.
+ *
+ * logp_i = z_i[t_i] - log sum over j of exp z_i[j]   for row i of the logits and its target t_i
+ * loss   = sum over i of weight_i l_i,   dlogits_i = weight_i dl_i/dlogp_i (onehot(t_i) - softmax(z_i))
+ * l = -logp where policy is NULL (negative log-likelihood), else with r = exp(logp - old_logp), a = advantage:
+ *   l = -min(r a, clip(r, 1 - clip_low, 1 + clip_high) a) + kl (exp(d) - d - 1),   d = ref_logp - logp
+ * (on the border of the range, and where a is 0, the gradient is that of r a).
+ * logits    in, device, rows x vocab of `type`, row i at element i*ld (ld >= vocab), aligned to its element
+ * targets   in, device, int64: a target outside 0 .. vocab-1 is a token that does not count
+ * weights   in, device, fp32, or NULL = 1.  A token that does not count or has a weight of 0 adds nothing to the loss, whatever its
+ *           logits and its policy inputs are, and its gradient is zero; its logp is 0 where it does not count
+ * loss      out, device, float[1], or NULL;  logp: out, device, float[rows], or NULL (both of the logits given, before any update)
+ * dlogits   out, device, of `type`, rows x vocab, row i at element i*ldd, or NULL; may be logits itself (with ldd = ld)
+ * workspace device, sl_token_loss_workspace_bytes(rows), 16-byte aligned; may be NULL where loss is
+ * 0 <= clip_low <= 1, clip_high >= 0, kl >= 0, finite; ref_logp may be NULL where kl is 0.  rows <= 2^21, 1 <= vocab <= 2^24.
+ * Exponentials are fp32, everything that a token has one of is formed in fp64. */
+typedef struct {
+    const float *old_logp, *advantage, *ref_logp;      /* device, one per row */
+    double clip_low, clip_high, kl;
+} sl_policy;
+size_t sl_token_loss_workspace_bytes(int64_t rows);
+int sl_token_loss(const void *logits, int type, int64_t ld, int64_t rows, int64_t vocab, const int64_t *targets, const float *weights,
+                  const sl_policy *policy, float *loss, float *logp, void *dlogits, int64_t ldd, void *workspace, void *stream);
+
+/* ---- Attention over packed sequences.
+ *
+ * Sequence s has the queries q_start[s] .. q_start[s+1] - 1 and the first k_count[s] of the keys k_start[s] .. k_start[s+1] - 1 (all of
+ * them where k_count is NULL).  With causal, query i of n sees key j of m where j <= i + m - n: the last query sees every key.
+ *   S = scale q k^T ;  P = softmax over the keys that a query sees ;  out = P v ;  lse = log of the sum of exp S
+ * A query that sees no key has out = 0 and lse = -infinity, and adds nothing to any gradient.
+ * Query head h reads key head h / (heads / kv_heads).  All tensors are bf16, tokens x heads x head_dim; scores, statistics and sums are fp32,
+ * probabilities and dS are rounded to bf16 on their way into the matrix unit.
+ * What lies outside the sequences - tokens before the first or behind the last, unused rows of a cache - is neither read into
+ * any result nor written.  An infinity or a NaN in a sequence can reach all of that sequence's results, of no other one's.
+ * Starts that do not ascend or point outside the tokens are cut off at the tokens' ends: no access leaves the tensors. */
+typedef struct {
+    int64_t sequences, tokens_q, tokens_k;     /* tokens: rows that the tensors have, <= 2^30 */
+    int32_t heads, kv_heads, head_dim;         /* heads a multiple of kv_heads, head_dim a multiple of 8 up to 128 */
+    int32_t causal;
+    double scale;                              /* > 0 */
+    const int32_t *q_start, *k_start;          /* device, sequences + 1; they may be the same */
+    const int32_t *k_count;                    /* device, sequences, or NULL */
+} sl_attention_shape;
+typedef struct {                               /* element (t, h, d) at data + t*token_stride + h*head_stride + d, in elements */
+    void *data;                                /* device, 16-byte aligned */
+    int64_t token_stride, head_stride;         /* multiples of 8, token_stride <= 2^24; no two rows of an output share memory */
+} sl_heads;
+/* lse: out, device, fp32, heads x tokens_q, or NULL.  (tokens / 128 + sequences) * heads is less than 2^24. */
+int sl_attention(const sl_attention_shape *shape, const sl_heads *q, const sl_heads *k, const sl_heads *v, const sl_heads *out, float *lse,
+                 void *stream);
+/* Gradients from that of out: dq like q, dk and dv like k and v, each summed over the heads that share it, in a fixed order.
+ * out, lse   in, as sl_attention left them;  workspace: device, sl_attention_workspace_bytes, 16-byte aligned */
+size_t sl_attention_workspace_bytes(int64_t tokens_q, int64_t heads);
+int sl_attention_backward(const sl_attention_shape *shape, const sl_heads *q, const sl_heads *k, const sl_heads *v, const sl_heads *out,
+                          const float *lse, const sl_heads *dout, const sl_heads *dq, const sl_heads *dk, const sl_heads *dv, void *workspace,
+                          void *stream);
+/* One new token per sequence (generation): query s is sequence s's and sees all of its keys; tokens_q = sequences, q_start and causal
+ * are not looked at.  workspace: device, 16-byte aligned; that of the largest call serves calls with fewer sequences and tokens. */
+size_t sl_attention_token_workspace_bytes(int64_t sequences, int64_t tokens_k, int heads, int kv_heads, int head_dim);
+int sl_attention_token(const sl_attention_shape *shape, const sl_heads *q, const sl_heads *k, const sl_heads *v, const sl_heads *out, void *workspace,
+                       void *stream);
+
 /* Per-kernel timing for benchmarks.  Between sl_profile_begin and
  * sl_profile_end every sl_compress / sl_decompress_avg_apply call on the plan
  * records HIP events on its stream around each of its kernels (no

@@ -39,6 +39,10 @@ EXPORTS = [
     "sl_adamw_create", "sl_adamw_destroy", "sl_adamw_num_blocks", "sl_grad_norm_workspace_bytes", "sl_grad_norm",
     "sl_adamw_step", "sl_adamw_step8", "sl_adamw_state_values",
     "sl_mx4_bytes", "sl_mx4_quantize", "sl_mx4_dequantize", "sl_mx4_workspace_bytes", "sl_mx4_product", "sl_mx4_linear",
+    "sl_rms_norm", "sl_rms_norm_workspace_bytes", "sl_rms_norm_backward",
+    "sl_attention", "sl_attention_workspace_bytes", "sl_attention_backward",
+    "sl_attention_token_workspace_bytes", "sl_attention_token",
+    "sl_token_loss_workspace_bytes", "sl_token_loss",
 ]
 PROF_PHASES = ["select", "stats", "codes", "lut", "residual", "apply", "index"]
 
@@ -51,6 +55,21 @@ class SlTensor(C.Structure):
 class SlAdamwParams(C.Structure):
     _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
                 ("weight_decay", C.c_double), ("step", C.c_int64)]
+
+
+class SlPolicy(C.Structure):
+    _fields_ = [("old_logp", C.c_void_p), ("advantage", C.c_void_p), ("ref_logp", C.c_void_p),
+                ("clip_low", C.c_double), ("clip_high", C.c_double), ("kl", C.c_double)]
+
+
+class SlAttentionShape(C.Structure):
+    _fields_ = [("sequences", C.c_int64), ("tokens_q", C.c_int64), ("tokens_k", C.c_int64),
+                ("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("causal", C.c_int32),
+                ("scale", C.c_double), ("q_start", C.c_void_p), ("k_start", C.c_void_p), ("k_count", C.c_void_p)]
+
+
+class SlHeads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
 
 
 class SparseLoCoError(RuntimeError):
@@ -168,6 +187,27 @@ def lib():
         L.sl_mx4_product.argtypes = [vp, vp, i64, i64, i64, vp, i32, i64, i32, vp, vp]
         L.sl_mx4_linear.restype = i32
         L.sl_mx4_linear.argtypes = [vp, i32, i64, vp, i64, i64, i64, vp, i32, i64, vp, vp]
+        L.sl_rms_norm.restype = i32
+        L.sl_rms_norm.argtypes = [vp, i32, i64, vp, i64, vp, i32, i64, vp, i32, i64, i64, C.c_double, vp, i32, i64, vp, vp, vp, vp]
+        L.sl_rms_norm_workspace_bytes.restype = sz
+        L.sl_rms_norm_workspace_bytes.argtypes = [i64, i64]
+        L.sl_rms_norm_backward.restype = i32
+        L.sl_rms_norm_backward.argtypes = [vp, i32, i64, vp, i32, vp, vp, i32, i64, vp, i64, vp, i32, i64, vp, i32, i64, i64, vp, vp]
+        ps, ph = C.POINTER(SlAttentionShape), C.POINTER(SlHeads)
+        L.sl_attention.restype = i32
+        L.sl_attention.argtypes = [ps, ph, ph, ph, ph, vp, vp]
+        L.sl_attention_workspace_bytes.restype = sz
+        L.sl_attention_workspace_bytes.argtypes = [i64, i64]
+        L.sl_attention_backward.restype = i32
+        L.sl_attention_backward.argtypes = [ps, ph, ph, ph, ph, vp, ph, ph, ph, ph, vp, vp]
+        L.sl_attention_token_workspace_bytes.restype = sz
+        L.sl_attention_token_workspace_bytes.argtypes = [i64, i64, i32, i32, i32]
+        L.sl_attention_token.restype = i32
+        L.sl_attention_token.argtypes = [ps, ph, ph, ph, ph, vp, vp]
+        L.sl_token_loss_workspace_bytes.restype = sz
+        L.sl_token_loss_workspace_bytes.argtypes = [i64]
+        L.sl_token_loss.restype = i32
+        L.sl_token_loss.argtypes = [vp, i32, i64, i64, i64, vp, vp, C.POINTER(SlPolicy), vp, vp, vp, i64, vp, vp]
         L.sl_strerror.restype = C.c_char_p
         L.sl_strerror.argtypes = [i32]
         L.sl_last_hip_error.restype = C.c_char_p
@@ -681,3 +721,203 @@ def sl_mx4_linear(x: torch.Tensor, w: torch.Tensor, y: torch.Tensor, workspace: 
                              _stream_ptr(stream))
     if st:
         raise SparseLoCoError("sl_mx4_linear", st)
+
+
+def _same(what: str, t: Optional[torch.Tensor], shape, dtype=None) -> None:
+    if t is not None and (tuple(t.shape) != tuple(shape) or (dtype is not None and t.dtype != dtype)):
+        raise ValueError(f"{what}: expected {tuple(shape)}{'' if dtype is None else ' of ' + str(dtype)}, got {tuple(t.shape)} of {t.dtype}")
+
+
+def _on_current_device(*tensors: Optional[torch.Tensor]) -> None:
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"expected tensors on the current device ({here}), got one on {t.device}")
+
+
+@functools.lru_cache(maxsize=4096)
+def sl_rms_norm_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib().sl_rms_norm_workspace_bytes(int(rows), int(cols)))
+
+
+def alloc_rms_norm_workspace(rows: int, cols: int, device="cuda") -> torch.Tensor:
+    return torch.empty(max(16, sl_rms_norm_workspace_bytes(rows, cols)), dtype=torch.uint8, device=device)
+
+
+def sl_rms_norm(x: torch.Tensor, weight: torch.Tensor, y: Optional[torch.Tensor], residual: Optional[torch.Tensor] = None,
+                h: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
+                qt: Optional[torch.Tensor] = None, eps: float = 1e-5, stream=None) -> None:
+    """h = x + residual; y = h / rms(h) * weight, dense and (q, qt) as 4-bit matrices of its rows and columns; rstd = 1 / rms."""
+    xp, xt, rows, cols, ldx = _matrix(x)
+    rp, rt, ldr, hp, ht, ldh = None, 0, 0, None, 0, 0
+    if (residual is None) != (h is None):
+        raise ValueError("residual and h go together")
+    _same("weight", weight, (cols,))
+    _same("y", y, x.shape)
+    if h is not None:
+        _same("residual", residual, x.shape)
+        _same("h", h, x.shape, residual.dtype)
+        rp, rt, _, _, ldr = _matrix(residual)
+        hp, ht, _, _, ldh = _matrix(h)
+    yp, yt, ldy = None, 0, 0
+    if y is not None:
+        yp, yt, _, _, ldy = _matrix(y)
+    _on_current_device(x, weight, y, residual, h, rstd, q, qt)
+    st = lib().sl_rms_norm(xp, xt, ldx, rp, ldr, hp, ht, ldh, _dev_ptr(weight), _type_of(weight), rows, cols, float(eps), yp, yt, ldy,
+                           _room("rstd", rstd, rows, torch.float32), _mx4_ptr(q, rows, cols), _mx4_ptr(qt, cols, rows), _stream_ptr(stream))
+    if st:
+        raise SparseLoCoError("sl_rms_norm", st)
+
+
+def sl_rms_norm_backward(h: torch.Tensor, weight: torch.Tensor, rstd: torch.Tensor, dy: torch.Tensor, dx: torch.Tensor,
+                         dh: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                         accumulate: bool = False, stream=None) -> None:
+    """dx: gradient of x (and of the residual) from dy and from dh, which reaches h past the norm; dw: fp32, or None."""
+    hp, ht, rows, cols, ldh = _matrix(h)
+    _same("weight", weight, (cols,))
+    _same("dy", dy, h.shape)
+    _same("dx", dx, h.shape)
+    _same("dh", dh, h.shape, dx.dtype)
+    _same("dw", dw, (cols,), torch.float32)
+    gp, gt, _, _, ldg = _matrix(dy)
+    op, ot, _, _, ldo = _matrix(dx)
+    ip, ldi = None, 0
+    if dh is not None:
+        ip, _, _, _, ldi = _matrix(dh)
+    _on_current_device(h, weight, rstd, dy, dx, dh, dw, workspace)
+    st = lib().sl_rms_norm_backward(hp, ht, ldh, _dev_ptr(weight), _type_of(weight), _room("rstd", rstd, rows, torch.float32), gp, gt, ldg,
+                                    ip, ldi, op, ot, ldo, _dev_ptr(dw), int(accumulate), rows, cols,
+                                    _room("workspace", workspace, 0 if dw is None else sl_rms_norm_workspace_bytes(rows, cols), torch.uint8),
+                                    _stream_ptr(stream))
+    if st:
+        raise SparseLoCoError("sl_rms_norm_backward", st)
+
+
+def _heads(what: str, t: torch.Tensor, shape) -> SlHeads:
+    _same(what, t, shape, torch.bfloat16)
+    token, head, step = t.stride()
+    if not t.is_cuda or step != 1:
+        raise ValueError(f"{what}: expected a device tensor whose heads are contiguous")
+    return SlHeads(t.data_ptr(), token if shape[0] > 1 else 0, head if shape[1] > 1 else 0)
+
+
+def _starts(what: str, t: Optional[torch.Tensor], n: Optional[int] = None) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or t.dim() != 1 or t.numel() < 1 or (n is not None and t.numel() != n):
+        raise ValueError(f"{what}: expected {'at least one' if n is None else n} int32 values, got {tuple(t.shape)} of {t.dtype}")
+    return _dev_ptr(t)
+
+
+def _attention_shape(q, k, q_start, k_start, k_count, scale, causal) -> SlAttentionShape:
+    tokens_q, heads, dim = q.shape
+    tokens_k, kv_heads, _ = k.shape
+    n = k_start.numel() - 1
+    return SlAttentionShape(n, tokens_q, tokens_k, heads, kv_heads, dim, int(causal), dim ** -0.5 if scale is None else float(scale),
+                            _starts("q_start", q_start, n + 1), _starts("k_start", k_start), _starts("k_count", k_count, n))
+
+
+def sl_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, q_start: torch.Tensor,
+                 k_start: Optional[torch.Tensor] = None, k_count: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                 causal: bool = True, lse: Optional[torch.Tensor] = None, stream=None) -> None:
+    """q, out: (tokens, heads, dim), k, v: (tokens, kv_heads, dim), bf16; q_start, k_start: where each sequence begins, and the last one
+    ends (k_start None: q_start); k_count: how many of a sequence's keys are used; scale None: dim ** -0.5; lse: (heads, tokens) fp32."""
+    shape = _attention_shape(q, k, q_start, q_start if k_start is None else k_start, k_count, scale, causal)
+    _same("lse", lse, (q.shape[1], q.shape[0]), torch.float32)
+    _on_current_device(q, k, v, out, q_start, k_start, k_count, lse)
+    st = lib().sl_attention(shape, _heads("q", q, q.shape), _heads("k", k, k.shape), _heads("v", v, k.shape), _heads("out", out, q.shape),
+                            _dev_ptr(lse), _stream_ptr(stream))
+    if st:
+        raise SparseLoCoError("sl_attention", st)
+
+
+@functools.lru_cache(maxsize=4096)
+def sl_attention_workspace_bytes(tokens: int, heads: int) -> int:
+    return int(lib().sl_attention_workspace_bytes(int(tokens), int(heads)))
+
+
+def alloc_attention_workspace(tokens: int, heads: int, device="cuda") -> torch.Tensor:
+    return torch.empty(max(16, sl_attention_workspace_bytes(tokens, heads)), dtype=torch.uint8, device=device)
+
+
+def sl_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor, dout: torch.Tensor,
+                          dq: torch.Tensor, dk: torch.Tensor, dv: torch.Tensor, q_start: torch.Tensor,
+                          k_start: Optional[torch.Tensor] = None, k_count: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                          causal: bool = True, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dq, dk, dv from dout and what sl_attention was given and left."""
+    shape = _attention_shape(q, k, q_start, q_start if k_start is None else k_start, k_count, scale, causal)
+    _same("lse", lse, (q.shape[1], q.shape[0]), torch.float32)
+    _on_current_device(q, k, v, out, lse, dout, dq, dk, dv, q_start, k_start, k_count, workspace)
+    st = lib().sl_attention_backward(shape, _heads("q", q, q.shape), _heads("k", k, k.shape), _heads("v", v, k.shape),
+                                     _heads("out", out, q.shape), _dev_ptr(lse), _heads("dout", dout, q.shape), _heads("dq", dq, q.shape),
+                                     _heads("dk", dk, k.shape), _heads("dv", dv, k.shape),
+                                     _room("workspace", workspace, sl_attention_workspace_bytes(q.shape[0], q.shape[1]), torch.uint8),
+                                     _stream_ptr(stream))
+    if st:
+        raise SparseLoCoError("sl_attention_backward", st)
+
+
+@functools.lru_cache(maxsize=4096)
+def sl_attention_token_workspace_bytes(sequences: int, tokens_k: int, heads: int, kv_heads: int, dim: int) -> int:
+    return int(lib().sl_attention_token_workspace_bytes(int(sequences), int(tokens_k), int(heads), int(kv_heads), int(dim)))
+
+
+def alloc_attention_token_workspace(sequences: int, tokens_k: int, heads: int, kv_heads: int, dim: int, device="cuda") -> torch.Tensor:
+    return torch.empty(max(16, sl_attention_token_workspace_bytes(sequences, tokens_k, heads, kv_heads, dim)), dtype=torch.uint8, device=device)
+
+
+def sl_attention_token(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, k_start: torch.Tensor,
+                       k_count: Optional[torch.Tensor] = None, scale: Optional[float] = None, workspace: Optional[torch.Tensor] = None,
+                       stream=None) -> None:
+    """One query per sequence: q, out (sequences, heads, dim); k, v (tokens, kv_heads, dim), the caches of all sequences."""
+    shape = _attention_shape(q, k, None, k_start, k_count, scale, False)
+    _on_current_device(q, k, v, out, k_start, k_count, workspace)
+    st = lib().sl_attention_token(shape, _heads("q", q, q.shape), _heads("k", k, k.shape), _heads("v", v, k.shape), _heads("out", out, q.shape),
+                                  _room("workspace", workspace, sl_attention_token_workspace_bytes(q.shape[0], k.shape[0], q.shape[1], k.shape[1],
+                                                                                                  q.shape[2]), torch.uint8), _stream_ptr(stream))
+    if st:
+        raise SparseLoCoError("sl_attention_token", st)
+
+
+class Policy:
+    """What makes a token loss a policy step's: log probabilities under the policy that sampled the tokens, advantages, how far the ratio
+    may fall and rise, and (kl > 0) log probabilities under a reference.  One fp32 value per token."""
+
+    def __init__(self, old_logp: torch.Tensor, advantage: torch.Tensor, clip_low: float, clip_high: float,
+                 ref_logp: Optional[torch.Tensor] = None, kl: float = 0.0):
+        self.old_logp, self.advantage, self.clip_low, self.clip_high, self.ref_logp, self.kl = old_logp, advantage, clip_low, clip_high, ref_logp, kl
+
+
+@functools.lru_cache(maxsize=4096)
+def sl_token_loss_workspace_bytes(rows: int) -> int:
+    return int(lib().sl_token_loss_workspace_bytes(int(rows)))
+
+
+def alloc_token_loss_workspace(rows: int, device="cuda") -> torch.Tensor:
+    return torch.empty(max(16, sl_token_loss_workspace_bytes(rows)), dtype=torch.uint8, device=device)
+
+
+def sl_token_loss(logits: torch.Tensor, targets: torch.Tensor, weights: Optional[torch.Tensor], loss: Optional[torch.Tensor],
+                  logp: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None, policy: Optional[Policy] = None,
+                  workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """loss = sum of weight * (negative log-likelihood, or the policy's clipped ratio and KL term) over the rows of the logits."""
+    p, typ, rows, vocab, ld = _matrix(logits)
+    _same("targets", targets, (rows,), torch.int64)
+    _same("weights", weights, (rows,), torch.float32)
+    _same("logp", logp, (rows,), torch.float32)
+    _same("dlogits", dlogits, logits.shape, logits.dtype)
+    dp, ldd = None, 0
+    if dlogits is not None:
+        dp, _, _, _, ldd = _matrix(dlogits)
+    pol = None
+    if policy is not None:
+        for what in ("old_logp", "advantage", "ref_logp"):
+            _same(what, getattr(policy, what), (rows,), torch.float32)
+        _on_current_device(policy.old_logp, policy.advantage, policy.ref_logp)
+        pol = SlPolicy(_dev_ptr(policy.old_logp), _dev_ptr(policy.advantage), _dev_ptr(policy.ref_logp), policy.clip_low, policy.clip_high, policy.kl)
+    _on_current_device(logits, targets, weights, loss, logp, dlogits, workspace)
+    st = lib().sl_token_loss(p, typ, ld, rows, vocab, _dev_ptr(targets), _dev_ptr(weights), pol, _room("loss", loss, 1, torch.float32), _dev_ptr(logp),
+                             dp, ldd, _room("workspace", workspace, 0 if loss is None else sl_token_loss_workspace_bytes(rows), torch.uint8),
+                             _stream_ptr(stream))
+    if st:
+        raise SparseLoCoError("sl_token_loss", st)

@@ -10,7 +10,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libsparseloco.so")
 SOURCES = ["sl_api.hip", "sl_select.hip", "sl_select_kept.hip", "sl_select_group.hip", "sl_quant.hip", "sl_apply.hip", "sl_coded.hip", "sl_apply_coded.hip", "sl_apply_group.hip", "sl_outer.hip",
-           "sl_noalloc.hip", "sl_adamw.hip", "sl_mx4.hip", "sl_mx4_product.hip"]
+           "sl_noalloc.hip", "sl_adamw.hip", "sl_mx4.hip", "sl_mx4_product.hip",
+           "sl_rms_norm.hip", "sl_attention.hip", "sl_attention_token.hip", "sl_token_loss.hip"]
 OBJ_DIR = os.path.join(PKG, "_build")
 
 HIPCC_FLAGS = [

@@ -1,0 +1,417 @@
+// Attention over packed sequences, forward and backward.
+//   S = scale q k^T ;  P = softmax over the keys that a query sees ;  out = P v ;  lse = log sum exp S
+//   dP = dout v^T ;  dS = P (dP - sum dout out) ;  dq = scale dS k ;  dk = scale dS^T q ;  dv = P^T dout
+#include <algorithm>
+#include <cmath>
+
+#include "sl_attention.h"
+#include "sl_internal.h"
+
+namespace {
+
+const float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+
+struct AttendArgs {
+    SlSequences s;
+    SlRows q, k, v, out;
+    float *lse;
+};
+
+struct BackArgs {
+    SlSequences s;
+    SlRows q, k, v, out, dout, dq, dk, dv;
+    const float *lse;
+    float *stats;                // per query: lse in base 2, sum dout out; heads x tokens each
+};
+
+// ---- forward ----
+
+// 128 queries of one head, 32 to a wave, over 64 keys at a time, two stages of LDS.  The running maximum moves only where a row's new one is
+// more than 2^8 above it: the sum and the output then stay below 2^8 times their values, and the output's registers are scaled a
+// few times in all.
+template <int D>
+__global__ void __launch_bounds__(256, 2) k_attend(AttendArgs A)
+{
+    extern __shared__ __align__(16) unsigned char lds[];
+    constexpr int TILE = AT_TILE * 2 * D, STEPS = D / 16, BLOCKS = D / 32;
+    const SlItem item = sl_item(blockIdx.x, (unsigned)A.s.heads);
+    if (item.tile >= A.s.tiles) return;
+    // (the last queries see the most keys: first)
+    SlSpan at;
+    if (!sl_find_tile(A.s.q_start, A.s.n, A.s.tokens_q, AT_ROWS, A.s.tiles - 1 - item.tile, at)) return;
+    int k0, kn;
+    sl_rows_of(A.s.k_start, A.s.k_count, at.s, A.s.tokens_k, k0, kn);
+    const int lane = threadIdx.x & 63, wave = sl_uniform((int)(threadIdx.x >> 6)), half = lane >> 5;
+    const int head = (int)item.head, kv = head / A.s.group, shift = kn - at.count;
+    const int row = at.row0 + wave * 32 + (lane & 31), mine = min(row, at.count - 1);
+    sl_b8 q[STEPS];
+    sl_own_row<D>(A.q.p + (long long)(at.first + mine) * A.q.token + head * A.q.head, half, A.s.octets, q);
+
+    // keys that this row sees, the first and the last row of the wave, the last of the workgroup
+    const int sees = A.s.causal ? min(kn, mine + shift + 1) : kn;
+    const int fewest = A.s.causal ? min(kn, min(at.row0 + wave * 32, at.count - 1) + shift + 1) : kn;
+    const int most = A.s.causal ? min(kn, min(at.row0 + wave * 32 + 31, at.count - 1) + shift + 1) : kn;
+    const int all = A.s.causal ? min(kn, min(at.row0 + AT_ROWS - 1, at.count - 1) + shift + 1) : kn;
+    const unsigned char *k = A.k.p + (long long)k0 * A.k.token + kv * A.k.head, *v = A.v.p + (long long)k0 * A.v.token + kv * A.v.head;
+    SlTileLoad<D> lk, lv;
+    lk.setup(wave, lane, A.s.octets, A.k.token);
+    lv.setup(wave, lane, A.s.octets, A.v.token);
+    const unsigned lds0 = (unsigned)(unsigned long long)(__attribute__((address_space(3))) unsigned char *)lds;
+    const int plain = sl_plain_base<D>(lane), turned = sl_turned_base<D>(lane);
+
+    sl_f16 o[BLOCKS];
+#pragma unroll
+    for (int m = 0; m < BLOCKS; ++m) o[m] = sl_zero16();
+    float top = -INFINITY, ref = 0.0f, sum = 0.0f;      // the maximum that the exponents refer to, and it or 0
+    const int tiles = (max(all, 0) + AT_TILE - 1) / AT_TILE;
+    if (tiles > 0) {
+        lk.load(k, 0, kn, lds0, wave);
+        lv.load(v, 0, kn, lds0 + 2 * TILE, wave);
+    }
+#pragma unroll 1
+    for (int t = 0; t < tiles; ++t) {
+        wait_dma<0>();
+        stage_barrier();
+        if (t + 1 < tiles) {
+            const unsigned to = lds0 + (unsigned)((t + 1) & 1) * TILE;
+            lk.load(k, (t + 1) * AT_TILE, kn, to, wave);
+            lv.load(v, (t + 1) * AT_TILE, kn, to + 2 * TILE, wave);
+        }
+        if (t * AT_TILE >= most) continue;
+        const unsigned char *kt = lds + (t & 1) * TILE, *vt = kt + 2 * TILE;
+        sl_f16 s[2];
+        s[0] = s[1] = sl_zero16();
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+            s[0] = sl_mfma(sl_plain<D>(kt, plain, 0, i), q[i], s[0]);
+            s[1] = sl_mfma(sl_plain<D>(kt, plain, 1, i), q[i], s[1]);
+        }
+        if ((t + 1) * AT_TILE > fewest) {
+            const int left = sees - t * AT_TILE - 4 * half;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (32 * i + 8 * (e >> 2) + (e & 3) >= left) s[i][e] = -INFINITY;
+        }
+        float now = s[0][0];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) now = fmaxf(now, fmaxf(s[0][e], s[1][e]));
+        now = sl_both_max(now) * A.s.scale2;
+        if (sl_ballot(now > top + 8.0f)) {
+            const float next = fmaxf(top, now), to = next == -INFINITY ? 0.0f : next, by = __builtin_amdgcn_exp2f(top - to);
+            top = next, ref = to, sum = sum * by;
+#pragma unroll
+            for (int m = 0; m < BLOCKS; ++m)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[m][e] = o[m][e] * by;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                s[i][e] = __builtin_amdgcn_exp2f(fmaf(s[i][e], A.s.scale2, -ref));
+                sum = sum + s[i][e];
+            }
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const sl_b8 p = sl_operand(s[g >> 1], g & 1);
+#pragma unroll
+            for (int m = 0; m < BLOCKS; ++m) o[m] = sl_mfma(sl_turned<D>(vt, turned, m, g), p, o[m]);
+        }
+    }
+    sum = sl_both_sum(sum);
+    const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const bool there = row < at.count;
+    sl_put_row<D>(A.out.p + (long long)(at.first + mine) * A.out.token + head * A.out.head, there, half, A.s.octets, o, by);
+    if (A.lse && there && half == 0)
+        A.lse[(long long)head * A.s.tokens_q + at.first + mine] = sum == 0.0f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * LN2;
+}
+
+// ---- backward ----
+
+// dq: queries to lanes as in the forward pass; S and dP of 32 keys at a time.  It also leaves what the pass over keys needs of a query.
+// sum dout out is that of P dP, too: for queries that see few keys, whose dP - sum dout out is small beside its terms, it is taken from there,
+// in a pass over the keys in front.  From out, which is rounded, it moves the dS of all of a query's keys the same way, by its own
+// rounding's share of |dout| |out|, which does not average out over few keys (1024 tokens, N(0, 1.5) queries: dq's error 0.28 % of its norm
+// with it, 0.24 % with the sum, of which the roundings of dS and dq themselves are 0.24).
+enum { FEW_KEYS = 256 };
+
+template <int D>
+__global__ void __launch_bounds__(256, 2) k_back_q(BackArgs A)
+{
+    extern __shared__ __align__(16) unsigned char lds[];
+    constexpr int TILE = AT_TILE * 2 * D, STEPS = D / 16, BLOCKS = D / 32;
+    const SlItem item = sl_item(blockIdx.x, (unsigned)A.s.heads);
+    if (item.tile >= A.s.tiles) return;
+    SlSpan at;
+    if (!sl_find_tile(A.s.q_start, A.s.n, A.s.tokens_q, AT_ROWS, A.s.tiles - 1 - item.tile, at)) return;
+    int k0, kn;
+    sl_rows_of(A.s.k_start, A.s.k_count, at.s, A.s.tokens_k, k0, kn);
+    const int lane = threadIdx.x & 63, wave = sl_uniform((int)(threadIdx.x >> 6)), half = lane >> 5;
+    const int head = (int)item.head, kv = head / A.s.group, shift = kn - at.count;
+    const int row = at.row0 + wave * 32 + (lane & 31), mine = min(row, at.count - 1);
+    const long long token = at.first + mine;
+    sl_b8 q[STEPS], g[STEPS];
+    sl_own_row<D>(A.dout.p + token * A.dout.token + head * A.dout.head, half, A.s.octets, g);
+    float delta = 0.0f;
+    {
+        sl_own_row<D>(A.out.p + token * A.out.token + head * A.out.head, half, A.s.octets, q);
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) delta = fmaf((float)q[i][e], (float)g[i][e], delta);
+        delta = sl_both_sum(delta);
+    }
+    sl_own_row<D>(A.q.p + token * A.q.token + head * A.q.head, half, A.s.octets, q);
+    const float lse = A.lse[(long long)head * A.s.tokens_q + token], lse2 = lse == -INFINITY ? 0.0f : lse * LOG2E;
+    const int sees = A.s.causal ? min(kn, mine + shift + 1) : kn;
+    const int fewest = A.s.causal ? min(kn, min(at.row0 + wave * 32, at.count - 1) + shift + 1) : kn;
+    const int most = A.s.causal ? min(kn, min(at.row0 + wave * 32 + 31, at.count - 1) + shift + 1) : kn;
+    const int all = A.s.causal ? min(kn, min(at.row0 + AT_ROWS - 1, at.count - 1) + shift + 1) : kn;
+    const unsigned char *k = A.k.p + (long long)k0 * A.k.token + kv * A.k.head, *v = A.v.p + (long long)k0 * A.v.token + kv * A.v.head;
+    SlTileLoad<D> lk, lv;
+    lk.setup(wave, lane, A.s.octets, A.k.token);
+    lv.setup(wave, lane, A.s.octets, A.v.token);
+    const unsigned lds0 = (unsigned)(unsigned long long)(__attribute__((address_space(3))) unsigned char *)lds;
+    const int plain = sl_plain_base<D>(lane), turned = sl_turned_base<D>(lane);
+    sl_f16 dq[BLOCKS];
+#pragma unroll
+    for (int m = 0; m < BLOCKS; ++m) dq[m] = sl_zero16();
+    const int tiles = (max(all, 0) + AT_TILE - 1) / AT_TILE;
+    const bool few = (A.s.causal ? min(kn, at.row0 + shift + 1) : kn) <= FEW_KEYS;
+    float sum = 0.0f;
+    auto load = [&](int step) __attribute__((always_inline)) {
+        const unsigned to = lds0 + (unsigned)(step & 1) * TILE;
+        const int t = step < 0 ? step + tiles : step;
+        lk.load(k, t * AT_TILE, kn, to, wave);
+        lv.load(v, t * AT_TILE, kn, to + 2 * TILE, wave);
+    };
+    const int first = few ? -tiles : 0;          // (steps below 0: the pass in front)
+    if (tiles > 0) load(first);
+#pragma unroll 1
+    for (int step = first; step < tiles; ++step) {
+        wait_dma<0>();
+        stage_barrier();
+        if (step + 1 < tiles) load(step + 1);
+        if (step == 0 && few) delta = sl_both_sum(sum);
+        const int t = step < 0 ? step + tiles : step;
+        if (t * AT_TILE >= most) continue;
+        const unsigned char *kt = lds + (step & 1) * TILE, *vt = kt + 2 * TILE;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            sl_f16 s = sl_zero16(), dp = sl_zero16();
+#pragma unroll
+            for (int j = 0; j < STEPS; ++j) {
+                s = sl_mfma(sl_plain<D>(kt, plain, i, j), q[j], s);
+                dp = sl_mfma(sl_plain<D>(vt, plain, i, j), g[j], dp);
+            }
+            const float less = step < 0 ? 0.0f : delta;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], A.s.scale2, -lse2)) * (dp[e] - less);
+            if ((t + 1) * AT_TILE > fewest) {
+                const int left = sees - t * AT_TILE - 4 * half - 32 * i;
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (8 * (e >> 2) + (e & 3) >= left) s[e] = 0.0f;
+            }
+            if (step < 0) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sum = sum + s[e];
+                continue;
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const sl_b8 ds = sl_operand(s, j);
+#pragma unroll
+                for (int m = 0; m < BLOCKS; ++m) dq[m] = sl_mfma(sl_turned<D>(kt, turned, m, 2 * i + j), ds, dq[m]);
+            }
+        }
+    }
+    if (row < at.count && half == 0) {
+        float *to = A.stats + (long long)head * A.s.tokens_q + token;
+        to[0] = lse2;
+        to[(long long)A.s.heads * A.s.tokens_q] = delta;
+    }
+    sl_put_row<D>(A.dq.p + token * A.dq.token + head * A.dq.head, row < at.count, half, A.s.octets, dq, A.s.scale);
+}
+
+// dk and dv: 128 keys of one key head, 32 to a wave, over all queries of the heads that share it, 64 at a time; the sums over the heads are
+// made in registers, in their order.
+template <int D>
+__global__ void __launch_bounds__(256, 1) k_back_kv(BackArgs A)
+{
+    extern __shared__ __align__(16) unsigned char lds[];
+    constexpr int TILE = AT_TILE * 2 * D, STAGE = 2 * TILE + 512, STEPS = D / 16, BLOCKS = D / 32;
+    const int kv_heads = A.s.heads / A.s.group;
+    const SlItem item = sl_item(blockIdx.x, (unsigned)kv_heads);
+    if (item.tile >= A.s.tiles) return;
+    SlSpan at;                                   // (the first keys are seen by the most queries: first)
+    if (!sl_find_tile(A.s.k_start, A.s.n, A.s.tokens_k, AT_ROWS, item.tile, at)) return;
+    int q0, qn, k0, kn;
+    sl_rows_of(A.s.q_start, nullptr, at.s, A.s.tokens_q, q0, qn);
+    sl_rows_of(A.s.k_start, A.s.k_count, at.s, A.s.tokens_k, k0, kn);
+    if (at.row0 >= kn) return;
+    const int lane = threadIdx.x & 63, wave = sl_uniform((int)(threadIdx.x >> 6)), half = lane >> 5;
+    const int kv = (int)item.head, shift = kn - qn;
+    const int key = at.row0 + wave * 32 + (lane & 31), mine = min(key, kn - 1);
+    const long long token = k0 + mine;
+    sl_b8 k[STEPS], v[STEPS];
+    sl_own_row<D>(A.k.p + token * A.k.token + kv * A.k.head, half, A.s.octets, k);
+    sl_own_row<D>(A.v.p + token * A.v.token + kv * A.v.head, half, A.s.octets, v);
+    SlTileLoad<D> lq, lg;
+    lq.setup(wave, lane, A.s.octets, A.q.token);
+    lg.setup(wave, lane, A.s.octets, A.dout.token);
+    const unsigned lds0 = (unsigned)(unsigned long long)(__attribute__((address_space(3))) unsigned char *)lds;
+    const int plain = sl_plain_base<D>(lane), turned = sl_turned_base<D>(lane);
+    sl_f16 dk[BLOCKS], dv[BLOCKS];
+#pragma unroll
+    for (int m = 0; m < BLOCKS; ++m) dk[m] = dv[m] = sl_zero16();
+    // the first query that sees a key of the workgroup, of the wave; the first that sees all of the wave's
+    const int first = A.s.causal ? max(at.row0 - shift, 0) / AT_TILE : 0, tiles = (qn + AT_TILE - 1) / AT_TILE;
+    const int wave_first = A.s.causal ? at.row0 + wave * 32 - shift : 0, wave_all = A.s.causal ? wave_first + 31 : 0;
+    const int per_head = max(tiles - first, 0), stages = per_head * A.s.group;
+    auto load = [&](int i) __attribute__((always_inline)) {
+        const int head = kv * A.s.group + i / per_head, tile = (first + i % per_head) * AT_TILE;
+        const unsigned to = lds0 + (unsigned)(i & 1) * STAGE;
+        lq.load(A.q.p + (long long)q0 * A.q.token + head * A.q.head, tile, qn, to, wave);
+        lg.load(A.dout.p + (long long)q0 * A.dout.token + head * A.dout.head, tile, qn, to + TILE, wave);
+        if (wave < 2)
+            dma4(A.stats + ((long long)wave * A.s.heads + head) * A.s.tokens_q + q0 + tile, (unsigned)min(lane, qn - 1 - tile) * 4u, to + 2 * TILE + wave * 256);
+    };
+    if (stages > 0) load(0);
+#pragma unroll 1
+    for (int n = 0; n < stages; ++n) {
+        wait_dma<0>();
+        stage_barrier();
+        if (n + 1 < stages) load(n + 1);
+        const int tile = (first + n % per_head) * AT_TILE;
+        const unsigned char *qt = lds + (n & 1) * STAGE, *gt = qt + TILE;
+        const float *stats = reinterpret_cast<const float *>(qt + 2 * TILE);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int row0 = tile + 32 * i;
+            if (row0 >= qn || row0 + 31 < wave_first) continue;
+            sl_f16 s = sl_zero16(), dp = sl_zero16();
+#pragma unroll
+            for (int j = 0; j < STEPS; ++j) {
+                s = sl_mfma(sl_plain<D>(qt, plain, i, j), k[j], s);
+                dp = sl_mfma(sl_plain<D>(gt, plain, i, j), v[j], dp);
+            }
+            sl_f4 lse[4], delta[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                lse[j] = *reinterpret_cast<const sl_f4 *>(stats + 32 * i + 8 * j + 4 * half);
+                delta[j] = *reinterpret_cast<const sl_f4 *>(stats + 64 + 32 * i + 8 * j + 4 * half);
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], A.s.scale2, -lse[e >> 2][e & 3]));
+                dp[e] = s[e] * (dp[e] - delta[e >> 2][e & 3]);
+            }
+            if (row0 + 32 > qn || row0 < wave_all) {
+                // query row0 + 4 half + 8 (e / 4) + e % 4: at least `from` and less than qn
+                const int from = (A.s.causal ? key - shift : 0) - row0 - 4 * half, end = qn - row0 - 4 * half;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int at_row = 8 * (e >> 2) + (e & 3);
+                    if (at_row < from || at_row >= end) s[e] = dp[e] = 0.0f;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const sl_b8 p = sl_operand(s, j), ds = sl_operand(dp, j);
+#pragma unroll
+                for (int m = 0; m < BLOCKS; ++m) {
+                    dv[m] = sl_mfma(sl_turned<D>(gt, turned, m, 2 * i + j), p, dv[m]);
+                    dk[m] = sl_mfma(sl_turned<D>(qt, turned, m, 2 * i + j), ds, dk[m]);
+                }
+            }
+        }
+    }
+    sl_put_row<D>(A.dk.p + token * A.dk.token + kv * A.dk.head, key < kn, half, A.s.octets, dk, A.s.scale);
+    sl_put_row<D>(A.dv.p + token * A.dv.token + kv * A.dv.head, key < kn, half, A.s.octets, dv, 1.0f);
+}
+
+int check_launch()
+{
+    const hipError_t err = hipGetLastError();
+    if (err == hipSuccess) return SL_OK;
+    sl_note_hip_error(err);
+    return SL_ERR_HIP;
+}
+
+template <class Args>
+int launch(void (*k)(Args), const Args &A, long long heads, unsigned lds, hipStream_t st)
+{
+    const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (err != hipSuccess) {
+        sl_note_hip_error(err);
+        return SL_ERR_HIP;
+    }
+    hipLaunchKernelGGL(k, dim3(sl_item_groups(A.s.tiles, heads)), dim3(256), lds, st, A);
+    return check_launch();
+}
+
+}  // namespace
+
+extern "C" {
+
+int sl_attention(const sl_attention_shape *shape, const sl_heads *q, const sl_heads *k, const sl_heads *v, const sl_heads *out, float *lse,
+                 void *stream)
+{
+    AttendArgs A = {};
+    if (!sl_attention_sequences(shape, A.s) || ((uintptr_t)lse & 3)) return SL_ERR_INVALID_ARG;
+    if (A.s.tokens_q == 0 || A.s.n == 0) return SL_OK;
+    const bool keys = A.s.tokens_k > 0;
+    const int64_t dim = shape->head_dim;
+    if (!shape->q_start || !sl_attention_in(q, true, A.q) || !sl_attention_in(k, keys, A.k) || !sl_attention_in(v, keys, A.v) ||
+        !sl_attention_out(out, true, A.s.tokens_q, A.s.heads, dim, A.out))
+        return SL_ERR_INVALID_ARG;
+    if (out->data == q->data || (keys && (out->data == k->data || out->data == v->data)) || out->data == (void *)lse) return SL_ERR_INVALID_ARG;
+    A.lse = lse;
+    A.s.tiles = (unsigned)A.s.tokens_q / AT_ROWS + (unsigned)A.s.n;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (A.s.octets <= 8) return launch(k_attend<64>, A, A.s.heads, 4 * AT_TILE * 2 * 64, st);
+    return launch(k_attend<128>, A, A.s.heads, 4 * AT_TILE * 2 * 128, st);
+}
+
+size_t sl_attention_workspace_bytes(int64_t tokens_q, int64_t heads)
+{
+    if (tokens_q < 1 || heads < 1 || tokens_q > AT_MOST_TOKENS || heads > AT_MOST_HEADS) return 0;
+    return 2 * sizeof(float) * (size_t)(tokens_q * heads);
+}
+
+int sl_attention_backward(const sl_attention_shape *shape, const sl_heads *q, const sl_heads *k, const sl_heads *v, const sl_heads *out,
+                          const float *lse, const sl_heads *dout, const sl_heads *dq, const sl_heads *dk, const sl_heads *dv, void *workspace,
+                          void *stream)
+{
+    BackArgs A = {};
+    if (!sl_attention_sequences(shape, A.s)) return SL_ERR_INVALID_ARG;
+    const bool queries = A.s.tokens_q > 0, keys = A.s.tokens_k > 0;
+    if (A.s.n == 0 || (!queries && !keys)) return SL_OK;
+    const int64_t dim = shape->head_dim, kv_heads = shape->kv_heads;
+    if (!shape->q_start || !sl_attention_in(q, queries, A.q) || !sl_attention_in(out, queries, A.out) || !sl_attention_in(dout, queries, A.dout) ||
+        !sl_attention_in(k, keys, A.k) || !sl_attention_in(v, keys, A.v) || !sl_attention_out(dq, queries, A.s.tokens_q, A.s.heads, dim, A.dq) ||
+        !sl_attention_out(dk, keys, A.s.tokens_k, kv_heads, dim, A.dk) || !sl_attention_out(dv, keys, A.s.tokens_k, kv_heads, dim, A.dv))
+        return SL_ERR_INVALID_ARG;
+    if (queries && (!lse || !workspace || ((uintptr_t)lse & 3) || ((uintptr_t)workspace & 15) || (const void *)lse == workspace)) return SL_ERR_INVALID_ARG;
+    const void *in[6] = {queries ? q->data : nullptr, queries ? out->data : nullptr, queries ? dout->data : nullptr, keys ? k->data : nullptr, keys ? v->data : nullptr, workspace};
+    const void *res[3] = {queries ? dq->data : nullptr, keys ? dk->data : nullptr, keys ? dv->data : nullptr};
+    for (int i = 0; i < 3; ++i)
+        for (int j = 0; res[i] && j < 6 + i; ++j)
+            if (res[i] == (j < 6 ? in[j] : res[j - 6])) return SL_ERR_INVALID_ARG;
+    A.lse = lse, A.stats = static_cast<float *>(workspace);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const bool narrow = A.s.octets <= 8;
+    const unsigned tile = AT_TILE * 2 * (narrow ? 64 : 128);
+    if (queries) {
+        A.s.tiles = (unsigned)A.s.tokens_q / AT_ROWS + (unsigned)A.s.n;
+        if (const int rc = launch(narrow ? k_back_q<64> : k_back_q<128>, A, A.s.heads, 4 * tile, st)) return rc;
+    }
+    if (!keys) return SL_OK;
+    A.s.tiles = (unsigned)A.s.tokens_k / AT_ROWS + (unsigned)A.s.n;
+    return launch(narrow ? k_back_kv<64> : k_back_kv<128>, A, A.s.heads / A.s.group, 4 * tile + 1024, st);
+}
+
+}  // extern "C"
