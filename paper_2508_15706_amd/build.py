@@ -21,6 +21,11 @@ HIPCC_FLAGS = [
     "-Wall", "-Wno-unused-function",
 ]
 
+# Matrix products whose results arithmetic reads: in vector registers, as far as those last; the compiler moves accumulators alone to the
+# accumulation registers then (left to itself, all of them, and every score is copied back; gradient of keys and values, 655 instructions in the
+# loop, so 568).
+EXTRA_FLAGS = {"sl_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+
 
 def hipcc() -> str:
     exe = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
@@ -48,7 +53,7 @@ def build_library(verbose: bool = False, extra=()) -> str:
     os.makedirs(OBJ_DIR, exist_ok=True)
     inc = ["-I", os.path.join(ROOT, "include"), "-I", CSRC]
     objs = [os.path.join(OBJ_DIR, s.replace(".hip", ".o")) for s in SOURCES]
-    cmds = [[hipcc(), *HIPCC_FLAGS, *extra, *inc, "-c", os.path.join(CSRC, s), "-o", o]
+    cmds = [[hipcc(), *HIPCC_FLAGS, *EXTRA_FLAGS.get(s, []), *extra, *inc, "-c", os.path.join(CSRC, s), "-o", o]
             for s, o in zip(SOURCES, objs)]
     with ThreadPoolExecutor(max_workers=min(8, len(cmds))) as pool:
         list(pool.map(lambda c: _run(c, verbose), cmds))

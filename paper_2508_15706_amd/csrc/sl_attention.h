@@ -66,6 +66,62 @@ SL_DEV bool sl_find_tile(const int *start, int n, int tokens, unsigned rows, uns
     out.s = lo, out.first = a, out.count = b - a, out.row0 = (int)row0;
     return row0 >= 0 && row0 < b - a;
 }
+// The same by work: where queries see only keys before them, a sequence's tile `level` from its light end is `level` tiles' work more than the
+// lightest, and a workgroup that begins with a heavy tile late keeps the others waiting.  Item t is the t-th of all sequences' tiles in
+// descending order of their levels.  Each lane holds PER sequences' numbers of tiles; the sum of max(tiles - level, 0) over them is
+// the number of tiles of that level or more.  Lists of more sequences than that have enough tiles for the order not to count.
+// (eight sequences of 2048 tokens, forward: 209 us in the sequences' order)
+template <int PER>
+SL_DEV bool sl_find_level(const int *start, int n, int tokens, unsigned rows, unsigned t, bool light_first, SlSpan &out)
+{
+    const int lane = threadIdx.x & 63;
+    int tiles[PER], most = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int s = i * 64 + lane;
+        const int a = s < n ? min(max(start[s], 0), tokens) : 0, b = s < n ? min(max(start[s + 1], a), tokens) : 0;
+        tiles[i] = (int)(((unsigned)(b - a) + rows - 1) / rows);
+        most = max(most, tiles[i]);
+    }
+    most = sl_uniform(sl_wave_max(most));
+    auto reach = [&](int level) __attribute__((always_inline)) {        // tiles of that level or more
+        int c = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) c += max(tiles[i] - level, 0);
+#pragma unroll
+        for (int l = 0; l < 6; ++l) c += sl_partner(c, l);
+        return (unsigned)sl_uniform(c);
+    };
+    int lo = 0, hi = most;                       // reach(lo) > t >= reach(hi)
+    if (reach(0) <= t) return false;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (reach(mid) > t) lo = mid;
+        else hi = mid;
+    }
+    unsigned left = t - reach(lo + 1);           // which of the sequences that have this level
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const unsigned long long has = sl_ballot(tiles[i] > lo);
+        const unsigned c = (unsigned)sl_popc(has);
+        if (left < c) {
+            const int s = sl_uniform(i * 64 + __builtin_ctzll(sl_ballot(tiles[i] > lo && (unsigned)sl_mbcnt(has) == left)));
+            const int a = min(max(start[s], 0), tokens), b = min(max(start[s + 1], a), tokens);
+            out.s = s, out.first = a, out.count = b - a;
+            out.row0 = (light_first ? lo : (int)(((unsigned)(b - a) + rows - 1) / rows) - 1 - lo) * (int)rows;
+            return true;
+        }
+        left -= c;
+    }
+    return false;
+}
+SL_DEV bool sl_find(const int *start, int n, int tokens, unsigned rows, unsigned tiles, unsigned t, bool light_first, SlSpan &out)
+{
+    if (n <= 64) return sl_find_level<1>(start, n, tokens, rows, t, light_first, out);
+    if (n <= 256) return sl_find_level<4>(start, n, tokens, rows, t, light_first, out);
+    return sl_find_tile(start, n, tokens, rows, light_first ? tiles - 1 - t : t, out);
+}
+
 // Rows of a sequence on one side; `count`: how many of them are used, or null.
 SL_DEV void sl_rows_of(const int *start, const int *count, int s, int tokens, int &first, int &n)
 {
@@ -76,10 +132,10 @@ SL_DEV void sl_rows_of(const int *start, const int *count, int s, int tokens, in
 
 // ---- tiles in LDS ----
 
-// Rows of D bf16 in pieces of 16 bytes; piece c of row r is at c ^ turn(r) of its row, so that neither eight rows' same piece nor
-// four rows' neighbouring ones meet in a bank.
+// Rows of D bf16 in pieces of 16 bytes; piece c of row r is at c ^ turn(r) of its row: eight consecutive rows' same piece, and four rows'
+// four neighbouring ones (what half a wave reads transposed), are in banks of their own.
 template <int D>
-SL_DEV int sl_turn(int r) { return D == 128 ? (r & 7) << 1 | (r >> 3 & 1) : (r >> 1 & 3) << 1 | (r >> 3 & 1); }
+SL_DEV int sl_turn(int r) { return D == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 3 & 1) << 1 | (r >> 2 & 1); }
 
 // One wave's share of 64 rows: 1 KB an instruction, every fourth from its own on.
 template <int D>
@@ -131,7 +187,7 @@ SL_DEV sl_b8 sl_turned(const unsigned char *tile, int base, int m, int g)
 {
     typedef short s4 __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) s4 *lds_s4;
-    const unsigned char *a = tile + (base ^ (m << 6)) + g * 16 * (2 * D), *b = tile + (base ^ (m << 6) ^ 16) + (g * 16 + 8) * (2 * D);
+    const unsigned char *a = tile + (base ^ (m << 6)) + g * 16 * (2 * D), *b = tile + (base ^ (m << 6) ^ 32) + (g * 16 + 8) * (2 * D);
     union { s4 h[2]; sl_b8 v; } u;
     u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(a));
     u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(b));
@@ -145,6 +201,20 @@ SL_DEV sl_f16 sl_zero16()
 #pragma unroll
     for (int i = 0; i < 16; ++i) z[i] = 0.0f;
     return z;
+}
+
+// The order of N products, each with one read of LDS: AHEAD reads first, then one for each product.  (Left to itself the compiler waits for
+// every pair of reads in front of its products: forward pass over 8192 tokens 390 us, so 315.)
+template <int N, int AHEAD>
+SL_DEV void sl_reads_ahead()
+{
+    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+    for (int i = 0; i < N - AHEAD; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
 }
 
 // Eight values of a score tile as the operand of the next product: rounded to bf16, which the matrix unit takes (half a step is

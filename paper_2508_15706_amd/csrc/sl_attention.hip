@@ -21,7 +21,9 @@ struct BackArgs {
     SlSequences s;
     SlRows q, k, v, out, dout, dq, dk, dv;
     const float *lse;
-    float *stats;                // per query: lse in base 2, sum dout out; heads x tokens each
+    float *stats;                // per query: lse in base 2, sum dout out; heads x tokens each.  Behind them what stands for no query: infinity, whose
+                                 // probabilities are 0, and 0
+    long long none;              // where
 };
 
 // ---- forward ----
@@ -36,9 +38,8 @@ __global__ void __launch_bounds__(256, 2) k_attend(AttendArgs A)
     constexpr int TILE = AT_TILE * 2 * D, STEPS = D / 16, BLOCKS = D / 32;
     const SlItem item = sl_item(blockIdx.x, (unsigned)A.s.heads);
     if (item.tile >= A.s.tiles) return;
-    // (the last queries see the most keys: first)
     SlSpan at;
-    if (!sl_find_tile(A.s.q_start, A.s.n, A.s.tokens_q, AT_ROWS, A.s.tiles - 1 - item.tile, at)) return;
+    if (!sl_find(A.s.q_start, A.s.n, A.s.tokens_q, AT_ROWS, A.s.tiles, item.tile, true, at)) return;
     int k0, kn;
     sl_rows_of(A.s.k_start, A.s.k_count, at.s, A.s.tokens_k, k0, kn);
     const int lane = threadIdx.x & 63, wave = sl_uniform((int)(threadIdx.x >> 6)), half = lane >> 5;
@@ -81,11 +82,14 @@ __global__ void __launch_bounds__(256, 2) k_attend(AttendArgs A)
         const unsigned char *kt = lds + (t & 1) * TILE, *vt = kt + 2 * TILE;
         sl_f16 s[2];
         s[0] = s[1] = sl_zero16();
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
             s[0] = sl_mfma(sl_plain<D>(kt, plain, 0, i), q[i], s[0]);
             s[1] = sl_mfma(sl_plain<D>(kt, plain, 1, i), q[i], s[1]);
         }
+        sl_reads_ahead<2 * STEPS, 8>();
+        __builtin_amdgcn_sched_barrier(0);
         if ((t + 1) * AT_TILE > fewest) {
             const int left = sees - t * AT_TILE - 4 * half;
 #pragma unroll
@@ -96,7 +100,7 @@ __global__ void __launch_bounds__(256, 2) k_attend(AttendArgs A)
         }
         float now = s[0][0];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) now = fmaxf(now, fmaxf(s[0][e], s[1][e]));
+        for (int e = 0; e < 16; ++e) now = __builtin_elementwise_maximum(now, __builtin_elementwise_maximum(s[0][e], s[1][e]));
         now = sl_both_max(now) * A.s.scale2;
         if (sl_ballot(now > top + 8.0f)) {
             const float next = fmaxf(top, now), to = next == -INFINITY ? 0.0f : next, by = __builtin_amdgcn_exp2f(top - to);
@@ -145,7 +149,7 @@ __global__ void __launch_bounds__(256, 2) k_back_q(BackArgs A)
     const SlItem item = sl_item(blockIdx.x, (unsigned)A.s.heads);
     if (item.tile >= A.s.tiles) return;
     SlSpan at;
-    if (!sl_find_tile(A.s.q_start, A.s.n, A.s.tokens_q, AT_ROWS, A.s.tiles - 1 - item.tile, at)) return;
+    if (!sl_find(A.s.q_start, A.s.n, A.s.tokens_q, AT_ROWS, A.s.tiles, item.tile, true, at)) return;
     int k0, kn;
     sl_rows_of(A.s.k_start, A.s.k_count, at.s, A.s.tokens_k, k0, kn);
     const int lane = threadIdx.x & 63, wave = sl_uniform((int)(threadIdx.x >> 6)), half = lane >> 5;
@@ -166,8 +170,6 @@ __global__ void __launch_bounds__(256, 2) k_back_q(BackArgs A)
     sl_own_row<D>(A.q.p + token * A.q.token + head * A.q.head, half, A.s.octets, q);
     const float lse = A.lse[(long long)head * A.s.tokens_q + token], lse2 = lse == -INFINITY ? 0.0f : lse * LOG2E;
     const int sees = A.s.causal ? min(kn, mine + shift + 1) : kn;
-    const int fewest = A.s.causal ? min(kn, min(at.row0 + wave * 32, at.count - 1) + shift + 1) : kn;
-    const int most = A.s.causal ? min(kn, min(at.row0 + wave * 32 + 31, at.count - 1) + shift + 1) : kn;
     const int all = A.s.causal ? min(kn, min(at.row0 + AT_ROWS - 1, at.count - 1) + shift + 1) : kn;
     const unsigned char *k = A.k.p + (long long)k0 * A.k.token + kv * A.k.head, *v = A.v.p + (long long)k0 * A.v.token + kv * A.v.head;
     SlTileLoad<D> lk, lv;
@@ -180,46 +182,58 @@ __global__ void __launch_bounds__(256, 2) k_back_q(BackArgs A)
     for (int m = 0; m < BLOCKS; ++m) dq[m] = sl_zero16();
     const int tiles = (max(all, 0) + AT_TILE - 1) / AT_TILE;
     const bool few = (A.s.causal ? min(kn, at.row0 + shift + 1) : kn) <= FEW_KEYS;
-    float sum = 0.0f;
-    auto load = [&](int step) __attribute__((always_inline)) {
+    auto load = [&](int step, int t) __attribute__((always_inline)) {
         const unsigned to = lds0 + (unsigned)(step & 1) * TILE;
-        const int t = step < 0 ? step + tiles : step;
         lk.load(k, t * AT_TILE, kn, to, wave);
         lv.load(v, t * AT_TILE, kn, to + 2 * TILE, wave);
     };
-    const int first = few ? -tiles : 0;          // (steps below 0: the pass in front)
-    if (tiles > 0) load(first);
-#pragma unroll 1
-    for (int step = first; step < tiles; ++step) {
-        wait_dma<0>();
-        stage_barrier();
-        if (step + 1 < tiles) load(step + 1);
-        if (step == 0 && few) delta = sl_both_sum(sum);
-        const int t = step < 0 ? step + tiles : step;
-        if (t * AT_TILE >= most) continue;
+    // P (dP - less) of half i of tile t
+    auto half_tile = [&](int step, int t, int i, float less) __attribute__((always_inline)) {
         const unsigned char *kt = lds + (step & 1) * TILE, *vt = kt + 2 * TILE;
+        sl_f16 s = sl_zero16(), dp = sl_zero16();
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            sl_f16 s = sl_zero16(), dp = sl_zero16();
+        for (int j = 0; j < STEPS; ++j) {
+            s = sl_mfma(sl_plain<D>(kt, plain, i, j), q[j], s);
+            dp = sl_mfma(sl_plain<D>(vt, plain, i, j), g[j], dp);
+        }
+        sl_reads_ahead<2 * STEPS, 6>();
+        __builtin_amdgcn_sched_barrier(0);
+        const int left = sees - t * AT_TILE - 4 * half - 32 * i;
 #pragma unroll
-            for (int j = 0; j < STEPS; ++j) {
-                s = sl_mfma(sl_plain<D>(kt, plain, i, j), q[j], s);
-                dp = sl_mfma(sl_plain<D>(vt, plain, i, j), g[j], dp);
-            }
-            const float less = step < 0 ? 0.0f : delta;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], A.s.scale2, -lse2)) * (dp[e] - less);
-            if ((t + 1) * AT_TILE > fewest) {
-                const int left = sees - t * AT_TILE - 4 * half - 32 * i;
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (8 * (e >> 2) + (e & 3) >= left) s[e] = 0.0f;
-            }
-            if (step < 0) {
+        for (int e = 0; e < 16; ++e) {
+            const float x = fmaf(s[e], A.s.scale2, -lse2);
+            s[e] = __builtin_amdgcn_exp2f(8 * (e >> 2) + (e & 3) < left ? x : -INFINITY) * (dp[e] - less);
+        }
+        return s;
+    };
+    int step = 0;
+    if (tiles > 0) load(0, 0);
+    if (few) {
+        float sum = 0.0f;
+#pragma unroll 1
+        for (int t = 0; t < tiles; ++t, ++step) {
+            wait_dma<0>();
+            stage_barrier();
+            load(step + 1, t + 1 < tiles ? t + 1 : 0);
+#pragma unroll 1
+            for (int i = 0; i < 2; ++i) {
+                const sl_f16 s = half_tile(step, t, i, 0.0f);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) sum = sum + s[e];
-                continue;
             }
+        }
+        delta = sl_both_sum(sum);
+    }
+#pragma unroll 1
+    for (int t = 0; t < tiles; ++t, ++step) {
+        wait_dma<0>();
+        stage_barrier();
+        if (t + 1 < tiles) load(step + 1, t + 1);
+        const unsigned char *kt = lds + (step & 1) * TILE;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const sl_f16 s = half_tile(step, t, i, delta);
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const sl_b8 ds = sl_operand(s, j);
@@ -228,6 +242,7 @@ __global__ void __launch_bounds__(256, 2) k_back_q(BackArgs A)
             }
         }
     }
+    if (blockIdx.x == 0 && threadIdx.x < 2) A.stats[A.none + threadIdx.x] = threadIdx.x == 0 ? INFINITY : 0.0f;
     if (row < at.count && half == 0) {
         float *to = A.stats + (long long)head * A.s.tokens_q + token;
         to[0] = lse2;
@@ -246,8 +261,8 @@ __global__ void __launch_bounds__(256, 1) k_back_kv(BackArgs A)
     const int kv_heads = A.s.heads / A.s.group;
     const SlItem item = sl_item(blockIdx.x, (unsigned)kv_heads);
     if (item.tile >= A.s.tiles) return;
-    SlSpan at;                                   // (the first keys are seen by the most queries: first)
-    if (!sl_find_tile(A.s.k_start, A.s.n, A.s.tokens_k, AT_ROWS, item.tile, at)) return;
+    SlSpan at;
+    if (!sl_find(A.s.k_start, A.s.n, A.s.tokens_k, AT_ROWS, A.s.tiles, item.tile, false, at)) return;
     int q0, qn, k0, kn;
     sl_rows_of(A.s.q_start, nullptr, at.s, A.s.tokens_q, q0, qn);
     sl_rows_of(A.s.k_start, A.s.k_count, at.s, A.s.tokens_k, k0, kn);
@@ -267,17 +282,19 @@ __global__ void __launch_bounds__(256, 1) k_back_kv(BackArgs A)
     sl_f16 dk[BLOCKS], dv[BLOCKS];
 #pragma unroll
     for (int m = 0; m < BLOCKS; ++m) dk[m] = dv[m] = sl_zero16();
-    // the first query that sees a key of the workgroup, of the wave; the first that sees all of the wave's
+    // the first query that sees a key of the workgroup, this lane's key
     const int first = A.s.causal ? max(at.row0 - shift, 0) / AT_TILE : 0, tiles = (qn + AT_TILE - 1) / AT_TILE;
-    const int wave_first = A.s.causal ? at.row0 + wave * 32 - shift : 0, wave_all = A.s.causal ? wave_first + 31 : 0;
+    const int key_first = A.s.causal ? key - shift : 0;
     const int per_head = max(tiles - first, 0), stages = per_head * A.s.group;
     auto load = [&](int i) __attribute__((always_inline)) {
         const int head = kv * A.s.group + i / per_head, tile = (first + i % per_head) * AT_TILE;
         const unsigned to = lds0 + (unsigned)(i & 1) * STAGE;
         lq.load(A.q.p + (long long)q0 * A.q.token + head * A.q.head, tile, qn, to, wave);
         lg.load(A.dout.p + (long long)q0 * A.dout.token + head * A.dout.head, tile, qn, to + TILE, wave);
-        if (wave < 2)
-            dma4(A.stats + ((long long)wave * A.s.heads + head) * A.s.tokens_q + q0 + tile, (unsigned)min(lane, qn - 1 - tile) * 4u, to + 2 * TILE + wave * 256);
+        if (wave < 2) {
+            const float *stats = A.stats + ((long long)wave * A.s.heads + head) * A.s.tokens_q + q0 + tile + lane;
+            dma4(tile + lane < qn ? stats : A.stats + A.none + wave, to + 2 * TILE + wave * 256);
+        }
     };
     if (stages > 0) load(0);
 #pragma unroll 1
@@ -287,47 +304,58 @@ __global__ void __launch_bounds__(256, 1) k_back_kv(BackArgs A)
         if (n + 1 < stages) load(n + 1);
         const int tile = (first + n % per_head) * AT_TILE;
         const unsigned char *qt = lds + (n & 1) * STAGE, *gt = qt + TILE;
-        const float *stats = reinterpret_cast<const float *>(qt + 2 * TILE);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int row0 = tile + 32 * i;
-            if (row0 >= qn || row0 + 31 < wave_first) continue;
-            sl_f16 s = sl_zero16(), dp = sl_zero16();
-#pragma unroll
-            for (int j = 0; j < STEPS; ++j) {
-                s = sl_mfma(sl_plain<D>(qt, plain, i, j), k[j], s);
-                dp = sl_mfma(sl_plain<D>(gt, plain, i, j), v[j], dp);
-            }
-            sl_f4 lse[4], delta[4];
+        const float *stats = reinterpret_cast<const float *>(qt + 2 * TILE) + 4 * half;
+        // 64 queries in 4 x STEPS steps of two products each: scores of the first 32, of the second, dk and dv of the first, of the second.
+        // There is one wave to a SIMD: while the matrix unit works on the second and third quarter the wave itself makes the first and the
+        // second half's exponentials, and operands are read AHEAD steps in front of their use.  The scheduler keeps the steps apart.
+        constexpr int AHEAD = 3, EACH = 16 / STEPS;
+        sl_f16 s[2], dp[2];
+        sl_b8 x[AHEAD + 1], y[AHEAD + 1], p[2][2], ds[2][2];
+        sl_f4 lse[2][4], delta[2][4];
+        s[0] = s[1] = dp[0] = dp[1] = sl_zero16();
+        auto fetch = [&](int n) __attribute__((always_inline)) {
+            const int r = n / STEPS, c = n % STEPS, to = n % (AHEAD + 1);
+            x[to] = r < 2 ? sl_plain<D>(qt, plain, r, c) : sl_turned<D>(gt, turned, c % BLOCKS, 2 * (r - 2) + c / BLOCKS);
+            y[to] = r < 2 ? sl_plain<D>(gt, plain, r, c) : sl_turned<D>(qt, turned, c % BLOCKS, 2 * (r - 2) + c / BLOCKS);
+        };
+        auto fetch_stats = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                lse[j] = *reinterpret_cast<const sl_f4 *>(stats + 32 * i + 8 * j + 4 * half);
-                delta[j] = *reinterpret_cast<const sl_f4 *>(stats + 64 + 32 * i + 8 * j + 4 * half);
+                lse[i][j] = *reinterpret_cast<const sl_f4 *>(stats + 32 * i + 8 * j);
+                delta[i][j] = *reinterpret_cast<const sl_f4 *>(stats + 64 + 32 * i + 8 * j);
             }
+        };
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], A.s.scale2, -lse[e >> 2][e & 3]));
-                dp[e] = s[e] * (dp[e] - delta[e >> 2][e & 3]);
+        for (int n = 0; n < AHEAD; ++n) fetch(n);
+        fetch_stats(0);
+#pragma unroll
+        for (int n = 0; n < 4 * STEPS; ++n) {
+            const int r = n / STEPS, c = n % STEPS, at = n % (AHEAD + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            if (n + AHEAD < 4 * STEPS) fetch(n + AHEAD);
+            if (n == STEPS) fetch_stats(1);
+            if (r < 2) {
+                s[r] = sl_mfma(x[at], k[c], s[r]);
+                dp[r] = sl_mfma(y[at], v[c], dp[r]);
+            } else {
+                dv[c % BLOCKS] = sl_mfma(x[at], p[r - 2][c / BLOCKS], dv[c % BLOCKS]);
+                dk[c % BLOCKS] = sl_mfma(y[at], ds[r - 2][c / BLOCKS], dk[c % BLOCKS]);
             }
-            if (row0 + 32 > qn || row0 < wave_all) {
-                // query row0 + 4 half + 8 (e / 4) + e % 4: at least `from` and less than qn
-                const int from = (A.s.causal ? key - shift : 0) - row0 - 4 * half, end = qn - row0 - 4 * half;
+            if (r == 1 || r == 2) {
+                const int i = r - 1, from = key_first - tile - 32 * i - 4 * half;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int at_row = 8 * (e >> 2) + (e & 3);
-                    if (at_row < from || at_row >= end) s[e] = dp[e] = 0.0f;
+                for (int e = c * EACH; e < (c + 1) * EACH; ++e) {
+                    // (a query that does not see the key: exp(-infinity))
+                    const float z = fmaf(s[i][e], A.s.scale2, -lse[i][e >> 2][e & 3]);
+                    s[i][e] = __builtin_amdgcn_exp2f(8 * (e >> 2) + (e & 3) < from ? -INFINITY : z);
+                    dp[i][e] = s[i][e] * (dp[i][e] - delta[i][e >> 2][e & 3]);
                 }
-            }
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const sl_b8 p = sl_operand(s, j), ds = sl_operand(dp, j);
-#pragma unroll
-                for (int m = 0; m < BLOCKS; ++m) {
-                    dv[m] = sl_mfma(sl_turned<D>(gt, turned, m, 2 * i + j), p, dv[m]);
-                    dk[m] = sl_mfma(sl_turned<D>(qt, turned, m, 2 * i + j), ds, dk[m]);
-                }
+                if (c == STEPS / 2 - 1) p[i][0] = sl_operand(s[i], 0), ds[i][0] = sl_operand(dp[i], 0);
+                if (c == STEPS - 1) p[i][1] = sl_operand(s[i], 1), ds[i][1] = sl_operand(dp[i], 1);
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
     }
     sl_put_row<D>(A.dk.p + token * A.dk.token + kv * A.dk.head, key < kn, half, A.s.octets, dk, A.s.scale);
     sl_put_row<D>(A.dv.p + token * A.dv.token + kv * A.dv.head, key < kn, half, A.s.octets, dv, 1.0f);
@@ -379,7 +407,7 @@ int sl_attention(const sl_attention_shape *shape, const sl_heads *q, const sl_he
 size_t sl_attention_workspace_bytes(int64_t tokens_q, int64_t heads)
 {
     if (tokens_q < 1 || heads < 1 || tokens_q > AT_MOST_TOKENS || heads > AT_MOST_HEADS) return 0;
-    return 2 * sizeof(float) * (size_t)(tokens_q * heads);
+    return sizeof(float) * (size_t)(2 * tokens_q * heads + 2);
 }
 
 int sl_attention_backward(const sl_attention_shape *shape, const sl_heads *q, const sl_heads *k, const sl_heads *v, const sl_heads *out,
@@ -401,7 +429,7 @@ int sl_attention_backward(const sl_attention_shape *shape, const sl_heads *q, co
     for (int i = 0; i < 3; ++i)
         for (int j = 0; res[i] && j < 6 + i; ++j)
             if (res[i] == (j < 6 ? in[j] : res[j - 6])) return SL_ERR_INVALID_ARG;
-    A.lse = lse, A.stats = static_cast<float *>(workspace);
+    A.lse = lse, A.stats = static_cast<float *>(workspace), A.none = 2ll * A.s.heads * A.s.tokens_q;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const bool narrow = A.s.octets <= 8;
     const unsigned tile = AT_TILE * 2 * (narrow ? 64 : 128);

@@ -12,10 +12,10 @@ SL_DEV void dma16(const unsigned char *base, unsigned lane_off, unsigned lds)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(lane_off), "s"(base) : "m0", "memory");
 }
-// The same with 4 bytes per lane, to `lds` + 4 * lane.
-SL_DEV void dma4(const void *base, unsigned lane_off, unsigned lds)
+// The same with 4 bytes per lane, each from an address of its own, to `lds` + 4 * lane.
+SL_DEV void dma4(const void *from, unsigned lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(lane_off), "s"(base) : "m0", "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(from) : "m0", "memory");
 }
 #pragma clang diagnostic pop
 template <int N>
