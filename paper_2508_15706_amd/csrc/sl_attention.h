@@ -137,10 +137,10 @@ SL_DEV void sl_rows_of(const int *start, const int *count, int s, int tokens, in
 template <int D>
 SL_DEV int sl_turn(int r) { return D == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 3 & 1) << 1 | (r >> 2 & 1); }
 
-// One wave's share of 64 rows: 1 KB an instruction, every fourth from its own on.
-template <int D>
+// One wave's share of ROWS rows: 1 KB an instruction, every fourth from its own on.
+template <int D, int ROWS = AT_TILE>
 struct SlTileLoad {
-    enum { PIECES = D / 8, PER = 64 / PIECES, LOADS = AT_TILE / PER / 4 };
+    enum { PIECES = D / 8, PER = 64 / PIECES, LOADS = ROWS / PER / 4 };
     int row;                     // this lane's in the first load
     unsigned at;                 // its piece's offset in a row
     unsigned off;                // its byte offset from the tile's first row
@@ -153,7 +153,7 @@ struct SlTileLoad {
         token = stride;
         off = (unsigned)row * (unsigned)token + at;
     }
-    // rows tile .. + 63 of `count`; what lies past the last one is read there
+    // rows tile .. + ROWS - 1 of `count`; what lies past the last one is read there
     SL_DEV void load(const unsigned char *base, int tile, int count, unsigned lds, int wave) const
     {
         const unsigned char *from = base + tile * token;
@@ -161,7 +161,7 @@ struct SlTileLoad {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const unsigned to = lds + (unsigned)(wave + 4 * i) * 1024u;
-            if (last >= AT_TILE - 1) dma16(from + i * (4 * PER) * token, off, to);
+            if (last >= ROWS - 1) dma16(from + i * (4 * PER) * token, off, to);
             else dma16(from, (unsigned)min(row + i * 4 * PER, last) * (unsigned)token + at, to);
         }
     }

@@ -251,13 +251,15 @@ __global__ void __launch_bounds__(256, 2) k_back_q(BackArgs A)
     sl_put_row<D>(A.dq.p + token * A.dq.token + head * A.dq.head, row < at.count, half, A.s.octets, dq, A.s.scale);
 }
 
-// dk and dv: 128 keys of one key head, 32 to a wave, over all queries of the heads that share it, 64 at a time; the sums over the heads are
-// made in registers, in their order.
+// dk and dv: 128 keys of one key head, 32 to a wave, over all queries of the heads that share it, 32 at a time; the sums over the heads are
+// made in registers, in their order.  A wave holds its keys in registers and its values in LDS, so that two workgroups fit a compute unit
+// and one's exponentials run beside the other's products.
+enum { AT_STAGE = 32 };
 template <int D>
-__global__ void __launch_bounds__(256, 1) k_back_kv(BackArgs A)
+__global__ void __launch_bounds__(256, 2) k_back_kv(BackArgs A)
 {
     extern __shared__ __align__(16) unsigned char lds[];
-    constexpr int TILE = AT_TILE * 2 * D, STAGE = 2 * TILE + 512, STEPS = D / 16, BLOCKS = D / 32;
+    constexpr int VALUES = AT_ROWS * 2 * D, TILE = AT_STAGE * 2 * D, STAGE = 2 * TILE + 256, STEPS = D / 16, BLOCKS = D / 32;
     const int kv_heads = A.s.heads / A.s.group;
     const SlItem item = sl_item(blockIdx.x, (unsigned)kv_heads);
     if (item.tile >= A.s.tiles) return;
@@ -271,92 +273,104 @@ __global__ void __launch_bounds__(256, 1) k_back_kv(BackArgs A)
     const int kv = (int)item.head, shift = kn - qn;
     const int key = at.row0 + wave * 32 + (lane & 31), mine = min(key, kn - 1);
     const long long token = k0 + mine;
-    sl_b8 k[STEPS], v[STEPS];
+    const unsigned lds0 = (unsigned)(unsigned long long)(__attribute__((address_space(3))) unsigned char *)lds;
+    {
+        SlTileLoad<D, AT_ROWS> lv;
+        lv.setup(wave, lane, A.s.octets, A.v.token);
+        lv.load(A.v.p + (long long)k0 * A.v.token + kv * A.v.head, at.row0, kn, lds0, wave);
+    }
+    sl_b8 k[STEPS];
     sl_own_row<D>(A.k.p + token * A.k.token + kv * A.k.head, half, A.s.octets, k);
-    sl_own_row<D>(A.v.p + token * A.v.token + kv * A.v.head, half, A.s.octets, v);
-    SlTileLoad<D> lq, lg;
+    SlTileLoad<D, AT_STAGE> lq, lg;
     lq.setup(wave, lane, A.s.octets, A.q.token);
     lg.setup(wave, lane, A.s.octets, A.dout.token);
-    const unsigned lds0 = (unsigned)(unsigned long long)(__attribute__((address_space(3))) unsigned char *)lds;
     const int plain = sl_plain_base<D>(lane), turned = sl_turned_base<D>(lane);
     sl_f16 dk[BLOCKS], dv[BLOCKS];
 #pragma unroll
     for (int m = 0; m < BLOCKS; ++m) dk[m] = dv[m] = sl_zero16();
-    // the first query that sees a key of the workgroup, this lane's key
-    const int first = A.s.causal ? max(at.row0 - shift, 0) / AT_TILE : 0, tiles = (qn + AT_TILE - 1) / AT_TILE;
-    const int key_first = A.s.causal ? key - shift : 0;
+    // the first query that sees a key of the workgroup, of the wave, this lane's key
+    const int first = A.s.causal ? max(at.row0 - shift, 0) / AT_STAGE : 0, tiles = (qn + AT_STAGE - 1) / AT_STAGE;
+    const int wave_first = A.s.causal ? at.row0 + wave * 32 - shift : 0, key_first = A.s.causal ? key - shift : 0;
     const int per_head = max(tiles - first, 0), stages = per_head * A.s.group;
     auto load = [&](int i) __attribute__((always_inline)) {
-        const int head = kv * A.s.group + i / per_head, tile = (first + i % per_head) * AT_TILE;
-        const unsigned to = lds0 + (unsigned)(i & 1) * STAGE;
+        const int head = kv * A.s.group + i / per_head, tile = (first + i % per_head) * AT_STAGE;
+        const unsigned to = lds0 + VALUES + (unsigned)(i & 1) * STAGE;
         lq.load(A.q.p + (long long)q0 * A.q.token + head * A.q.head, tile, qn, to, wave);
         lg.load(A.dout.p + (long long)q0 * A.dout.token + head * A.dout.head, tile, qn, to + TILE, wave);
-        if (wave < 2) {
-            const float *stats = A.stats + ((long long)wave * A.s.heads + head) * A.s.tokens_q + q0 + tile + lane;
-            dma4(tile + lane < qn ? stats : A.stats + A.none + wave, to + 2 * TILE + wave * 256);
+        if (wave == 0) {
+            const int row = tile + (lane & 31);
+            const float *stats = A.stats + ((long long)half * A.s.heads + head) * A.s.tokens_q + q0 + row;
+            dma4(row < qn ? stats : A.stats + A.none + half, to + 2 * TILE);
         }
     };
     if (stages > 0) load(0);
+    if (A.s.octets < D / 8) {
+        // (both operands of dP come out of LDS: one of them has to be zero past the last column)
+        wait_dma<0>();
+        __syncthreads();
+        const int pieces = D / 8 - A.s.octets;
+        for (int i = threadIdx.x; i < AT_ROWS * pieces; i += 256) {
+            const int r = i / pieces, c = A.s.octets + i % pieces;
+            *reinterpret_cast<sl_u4 *>(lds + r * (2 * D) + ((c ^ sl_turn<D>(r)) << 4)) = sl_u4{0u, 0u, 0u, 0u};
+        }
+    }
 #pragma unroll 1
     for (int n = 0; n < stages; ++n) {
         wait_dma<0>();
         stage_barrier();
         if (n + 1 < stages) load(n + 1);
-        const int tile = (first + n % per_head) * AT_TILE;
-        const unsigned char *qt = lds + (n & 1) * STAGE, *gt = qt + TILE;
+        const int tile = (first + n % per_head) * AT_STAGE;
+        if (tile + AT_STAGE <= wave_first) continue;
+        const unsigned char *qt = lds + VALUES + (n & 1) * STAGE, *gt = qt + TILE;
         const float *stats = reinterpret_cast<const float *>(qt + 2 * TILE) + 4 * half;
-        // 64 queries in 4 x STEPS steps of two products each: scores of the first 32, of the second, dk and dv of the first, of the second.
-        // There is one wave to a SIMD: while the matrix unit works on the second and third quarter the wave itself makes the first and the
-        // second half's exponentials, and operands are read AHEAD steps in front of their use.  The scheduler keeps the steps apart.
-        constexpr int AHEAD = 3, EACH = 16 / STEPS;
-        sl_f16 s[2], dp[2];
-        sl_b8 x[AHEAD + 1], y[AHEAD + 1], p[2][2], ds[2][2];
-        sl_f4 lse[2][4], delta[2][4];
-        s[0] = s[1] = dp[0] = dp[1] = sl_zero16();
-        auto fetch = [&](int n) __attribute__((always_inline)) {
-            const int r = n / STEPS, c = n % STEPS, to = n % (AHEAD + 1);
-            x[to] = r < 2 ? sl_plain<D>(qt, plain, r, c) : sl_turned<D>(gt, turned, c % BLOCKS, 2 * (r - 2) + c / BLOCKS);
-            y[to] = r < 2 ? sl_plain<D>(gt, plain, r, c) : sl_turned<D>(qt, turned, c % BLOCKS, 2 * (r - 2) + c / BLOCKS);
-        };
-        auto fetch_stats = [&](int i) __attribute__((always_inline)) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                lse[i][j] = *reinterpret_cast<const sl_f4 *>(stats + 32 * i + 8 * j);
-                delta[i][j] = *reinterpret_cast<const sl_f4 *>(stats + 64 + 32 * i + 8 * j);
-            }
-        };
+        sl_f16 s = sl_zero16(), dp = sl_zero16();
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int n = 0; n < AHEAD; ++n) fetch(n);
-        fetch_stats(0);
+        for (int j = 0; j < STEPS; ++j) s = sl_mfma(sl_plain<D>(qt, plain, 0, j), k[j], s);
 #pragma unroll
-        for (int n = 0; n < 4 * STEPS; ++n) {
-            const int r = n / STEPS, c = n % STEPS, at = n % (AHEAD + 1);
-            __builtin_amdgcn_sched_barrier(0);
-            if (n + AHEAD < 4 * STEPS) fetch(n + AHEAD);
-            if (n == STEPS) fetch_stats(1);
-            if (r < 2) {
-                s[r] = sl_mfma(x[at], k[c], s[r]);
-                dp[r] = sl_mfma(y[at], v[c], dp[r]);
-            } else {
-                dv[c % BLOCKS] = sl_mfma(x[at], p[r - 2][c / BLOCKS], dv[c % BLOCKS]);
-                dk[c % BLOCKS] = sl_mfma(y[at], ds[r - 2][c / BLOCKS], dk[c % BLOCKS]);
-            }
-            if (r == 1 || r == 2) {
-                const int i = r - 1, from = key_first - tile - 32 * i - 4 * half;
+        for (int j = 0; j < STEPS; ++j) dp = sl_mfma(sl_plain<D>(gt, plain, 0, j), sl_plain<D>(lds, plain, wave, j), dp);
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
-                for (int e = c * EACH; e < (c + 1) * EACH; ++e) {
-                    // (a query that does not see the key: exp(-infinity))
-                    const float z = fmaf(s[i][e], A.s.scale2, -lse[i][e >> 2][e & 3]);
-                    s[i][e] = __builtin_amdgcn_exp2f(8 * (e >> 2) + (e & 3) < from ? -INFINITY : z);
-                    dp[i][e] = s[i][e] * (dp[i][e] - delta[i][e >> 2][e & 3]);
-                }
-                if (c == STEPS / 2 - 1) p[i][0] = sl_operand(s[i], 0), ds[i][0] = sl_operand(dp[i], 0);
-                if (c == STEPS - 1) p[i][1] = sl_operand(s[i], 1), ds[i][1] = sl_operand(dp[i], 1);
+        for (int j = 0; j < STEPS; ++j) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+#pragma unroll
+        for (int j = 0; j < STEPS; ++j) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        const int from = key_first - tile - 4 * half;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const sl_f4 lse = *reinterpret_cast<const sl_f4 *>(stats + 8 * j), delta = *reinterpret_cast<const sl_f4 *>(stats + 32 + 8 * j);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                // (a query that does not see the key: exp(-infinity))
+                const float x = fmaf(s[4 * j + e], A.s.scale2, -lse[e]);
+                s[4 * j + e] = __builtin_amdgcn_exp2f(8 * j + e < from ? -INFINITY : x);
+                dp[4 * j + e] = s[4 * j + e] * (dp[4 * j + e] - delta[e]);
             }
         }
         __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const sl_b8 p = sl_operand(s, j), ds = sl_operand(dp, j);
+#pragma unroll
+            for (int m = 0; m < BLOCKS; ++m) {
+                dv[m] = sl_mfma(sl_turned<D>(gt, turned, m, j), p, dv[m]);
+                dk[m] = sl_mfma(sl_turned<D>(qt, turned, m, j), ds, dk[m]);
+            }
+        }
+        __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+#pragma unroll
+        for (int j = 0; j < 4 * BLOCKS; ++j) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
     }
+    wait_dma<0>();               // (the values, where there was no stage)
     sl_put_row<D>(A.dk.p + token * A.dk.token + kv * A.dk.head, key < kn, half, A.s.octets, dk, A.s.scale);
     sl_put_row<D>(A.dv.p + token * A.dv.token + kv * A.dv.head, key < kn, half, A.s.octets, dv, 1.0f);
 }
@@ -439,7 +453,7 @@ int sl_attention_backward(const sl_attention_shape *shape, const sl_heads *q, co
     }
     if (!keys) return SL_OK;
     A.s.tiles = (unsigned)A.s.tokens_k / AT_ROWS + (unsigned)A.s.n;
-    return launch(narrow ? k_back_kv<64> : k_back_kv<128>, A, A.s.heads / A.s.group, 4 * tile + 1024, st);
+    return launch(narrow ? k_back_kv<64> : k_back_kv<128>, A, A.s.heads / A.s.group, 4 * tile + 512, st);
 }
 
 }  // extern "C"
