@@ -18,7 +18,8 @@
 typedef float sl_f16 __attribute__((ext_vector_type(16)));
 typedef __bf16 sl_b8 __attribute__((ext_vector_type(8)));
 
-enum { AT_ROWS = 128, AT_TILE = 64 };      // rows of a workgroup, 32 to each of its waves; rows of the other side in a stage of LDS
+// Rows of a workgroup, 32 to each of its waves; rows of the other side in a stage of LDS, and in a short one.
+enum { AT_ROWS = 128, AT_TILE = 64, AT_STAGE = 32 };
 
 struct SlRows {                  // a tensor of tokens x heads x dim; strides in bytes
     unsigned char *p;
@@ -167,6 +168,37 @@ struct SlTileLoad {
     }
 };
 
+// 32 rows to a wave's own LDS.
+template <int D>
+struct SlWaveLoad {
+    enum { PIECES = D / 8, PER = 64 / PIECES, LOADS = AT_STAGE / PER };
+    unsigned at[LOADS], off[LOADS];
+    int row;
+    long long token;
+
+    SL_DEV void setup(int lane, int octets, long long stride)
+    {
+        row = lane / PIECES, token = stride;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            at[i] = (unsigned)min((lane % PIECES) ^ sl_turn<D>(row + i * PER), octets - 1) * 16u;
+            off[i] = (unsigned)(row + i * PER) * (unsigned)token + at[i];
+        }
+    }
+    // rows first .. + 31, of which `count` exist (at least one)
+    SL_DEV void load(const unsigned char *base, int first, int count, unsigned lds) const
+    {
+        const unsigned char *from = base + first * token;
+        if (count >= AT_STAGE) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) dma16(from, off[i], lds + i * 1024u);
+        } else {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) dma16(from, (unsigned)min(row + i * PER, count - 1) * (unsigned)token + at[i], lds + i * 1024u);
+        }
+    }
+};
+
 // Operand with rows of the tile as its rows (or columns): step s, 16 of D, of rows 32 t + l % 32.
 template <int D>
 SL_DEV int sl_plain_base(int lane) { return (lane & 31) * (2 * D) + (((lane >> 5) ^ sl_turn<D>(lane & 31)) << 4); }
@@ -238,6 +270,52 @@ SL_DEV float sl_both_sum(float v)
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// One wave's softmax over 32 keys at a time.  The maximum that the exponents refer to moves only where a row's new one is more than 2^8 above
+// it: the sum and the output then stay below 2^8 times their values, and the output's registers are scaled a few times in all.
+struct SlRunning {
+    float top = -INFINITY, ref = 0.0f, sum = 0.0f;       // the maximum, it or 0, this half's part of the sum
+
+    // keys 8 g + e >= left of this half are not seen
+    template <int D>
+    SL_DEV void tile(const unsigned char *kt, const unsigned char *vt, int plain, int turned, const sl_b8 (&q)[D / 16], int left, float scale2, sl_f16 (&o)[D / 32])
+    {
+        sl_f16 s = sl_zero16();
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) s = sl_mfma(sl_plain<D>(kt, plain, 0, i), q[i], s);
+        sl_reads_ahead<D / 16, 4>();
+        __builtin_amdgcn_sched_barrier(0);
+        if (sl_ballot(left < AT_STAGE - 4)) {                // (the last key of either half is its 27th)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (8 * (e >> 2) + (e & 3) >= left) s[e] = -INFINITY;
+        }
+        float now = s[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) now = __builtin_elementwise_maximum(now, s[e]);
+        now = sl_both_max(now) * scale2;
+        if (sl_ballot(now > top + 8.0f)) {
+            const float next = fmaxf(top, now), to = next == -INFINITY ? 0.0f : next, by = __builtin_amdgcn_exp2f(top - to);
+            top = next, ref = to, sum = sum * by;
+#pragma unroll
+            for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[m][e] = o[m][e] * by;
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], scale2, -ref));
+            sum = sum + s[e];
+        }
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const sl_b8 p = sl_operand(s, g);
+#pragma unroll
+            for (int m = 0; m < D / 32; ++m) o[m] = sl_mfma(sl_turned<D>(vt, turned, m, g), p, o[m]);
+        }
+    }
+};
+
 // Row of a wave's own side: 16 bytes at every other piece, this half's.
 template <int D>
 SL_DEV void sl_own_row(const unsigned char *row, int half, int octets, sl_b8 (&v)[D / 16])
@@ -250,21 +328,44 @@ SL_DEV void sl_own_row(const unsigned char *row, int half, int octets, sl_b8 (&v
     }
 }
 
-// A transposed result (rows of D, this lane's column a row of memory) times `by`, in bf16: the halves exchange every second four so that
+// 32 columns of a transposed result (this lane's column a row of memory) times `by`, in bf16: the halves exchange every second four so that
 // each writes 16 bytes.
+SL_DEV void sl_put_block(unsigned char *row, bool there, int half, int octets, const sl_f16 &v, int m, float by)
+{
+#pragma unroll
+    for (int g = 0; g < 4; g += 2) {
+        const unsigned a0 = sl_bf16_pair(v[4 * g] * by, v[4 * g + 1] * by), a1 = sl_bf16_pair(v[4 * g + 2] * by, v[4 * g + 3] * by);
+        const unsigned b0 = sl_bf16_pair(v[4 * g + 4] * by, v[4 * g + 5] * by), b1 = sl_bf16_pair(v[4 * g + 6] * by, v[4 * g + 7] * by);
+        const auto r0 = __builtin_amdgcn_permlane32_swap(a0, b0, false, false), r1 = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
+        const int piece = m * 4 + g + half;
+        if (there && piece < octets) *reinterpret_cast<sl_u4 *>(row + piece * 16) = sl_u4{r0[0], r1[0], r0[1], r1[1]};
+    }
+}
 template <int D>
 SL_DEV void sl_put_row(unsigned char *row, bool there, int half, int octets, const sl_f16 (&v)[D / 32], float by)
 {
 #pragma unroll
-    for (int m = 0; m < D / 32; ++m)
+    for (int m = 0; m < D / 32; ++m) sl_put_block(row, there, half, octets, v[m], m, by);
+}
+
+// A wave's block of a result to LDS and the sum of four waves' from there, in their order; 16 floats a lane, 4 KB a block.
+SL_DEV void sl_leave_block(float *room, int lane, const sl_f16 &v)
+{
 #pragma unroll
-        for (int g = 0; g < 4; g += 2) {
-            const unsigned a0 = sl_bf16_pair(v[m][4 * g] * by, v[m][4 * g + 1] * by), a1 = sl_bf16_pair(v[m][4 * g + 2] * by, v[m][4 * g + 3] * by);
-            const unsigned b0 = sl_bf16_pair(v[m][4 * g + 4] * by, v[m][4 * g + 5] * by), b1 = sl_bf16_pair(v[m][4 * g + 6] * by, v[m][4 * g + 7] * by);
-            const auto r0 = __builtin_amdgcn_permlane32_swap(a0, b0, false, false), r1 = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
-            const int piece = m * 4 + g + half;
-            if (there && piece < octets) *reinterpret_cast<sl_u4 *>(row + piece * 16) = sl_u4{r0[0], r1[0], r0[1], r1[1]};
+    for (int j = 0; j < 4; ++j) *reinterpret_cast<sl_f4 *>(room + j * 256 + lane * 4) = sl_f4{v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
+}
+SL_DEV sl_f16 sl_four_blocks(const float *room, int stride, int lane, sl_f4 by)
+{
+    sl_f16 v = sl_zero16();
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const sl_f4 x = *reinterpret_cast<const sl_f4 *>(room + w * stride + j * 256 + lane * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[4 * j + e] = fmaf(x[e], by[w], v[4 * j + e]);
         }
+    return v;
 }
 
 // ---- arguments ----

@@ -132,6 +132,82 @@ __global__ void __launch_bounds__(256, 2) k_attend(AttendArgs A)
         A.lse[(long long)head * A.s.tokens_q + at.first + mine] = sum == 0.0f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * LN2;
 }
 
+// Few tiles: 32 queries to a workgroup, whose four waves take every fourth 32 keys, in LDS of their own, and wait for nobody; their sums meet
+// at the end.
+template <int D>
+__global__ void __launch_bounds__(256, 1) k_attend_few(AttendArgs A)
+{
+    extern __shared__ __align__(16) unsigned char lds[];
+    constexpr int TILE = AT_STAGE * 2 * D, STEPS = D / 16, BLOCKS = D / 32, LOADS = 2 * SlWaveLoad<D>::LOADS;
+    const SlItem item = sl_item(blockIdx.x, (unsigned)A.s.heads);
+    if (item.tile >= A.s.tiles) return;
+    SlSpan at;
+    if (!sl_find(A.s.q_start, A.s.n, A.s.tokens_q, 32, A.s.tiles, item.tile, true, at)) return;
+    int k0, kn;
+    sl_rows_of(A.s.k_start, A.s.k_count, at.s, A.s.tokens_k, k0, kn);
+    const int lane = threadIdx.x & 63, wave = sl_uniform((int)(threadIdx.x >> 6)), half = lane >> 5;
+    const int head = (int)item.head, kv = head / A.s.group, shift = kn - at.count;
+    const int row = at.row0 + (lane & 31), mine = min(row, at.count - 1);
+    const unsigned char *k = A.k.p + (long long)k0 * A.k.token + kv * A.k.head, *v = A.v.p + (long long)k0 * A.v.token + kv * A.v.head;
+    SlWaveLoad<D> lk, lv;
+    lk.setup(lane, A.s.octets, A.k.token);
+    lv.setup(lane, A.s.octets, A.v.token);
+    unsigned char *own = lds + wave * (4 * TILE);
+    const unsigned lds0 = (unsigned)(unsigned long long)(__attribute__((address_space(3))) unsigned char *)own;
+    // keys that this row sees, the first row of the workgroup, its last
+    const int sees = A.s.causal ? min(kn, mine + shift + 1) : kn, fewest = A.s.causal ? min(kn, at.row0 + shift + 1) : kn;
+    const int all = A.s.causal ? min(kn, min(at.row0 + 31, at.count - 1) + shift + 1) : kn;
+    const int tiles = (max(all, 0) + AT_STAGE - 1) / AT_STAGE, steps = tiles > wave ? (tiles - wave + 3) / 4 : 0;
+    // (past the last step it brings that one again, so that every step waits for the same number of loads)
+    auto fill = [&](int i) __attribute__((always_inline)) {
+        const int from = (wave + 4 * min(i, steps - 1)) * AT_STAGE;
+        const unsigned to = lds0 + (unsigned)(i & 1) * (2 * TILE);
+        lk.load(k, from, kn - from, to);
+        lv.load(v, from, kn - from, to + TILE);
+    };
+    if (steps > 0) fill(0), fill(1);
+    sl_b8 q[STEPS];
+    sl_own_row<D>(A.q.p + (long long)(at.first + mine) * A.q.token + head * A.q.head, half, A.s.octets, q);
+    const int plain = sl_plain_base<D>(lane), turned = sl_turned_base<D>(lane);
+    sl_f16 o[BLOCKS];
+#pragma unroll
+    for (int m = 0; m < BLOCKS; ++m) o[m] = sl_zero16();
+    SlRunning run;
+#pragma unroll 1
+    for (int t = 0; t < steps; ++t) {
+        wait_dma<LOADS>();
+        const unsigned char *kt = own + (t & 1) * (2 * TILE);
+        const int first = (wave + 4 * t) * AT_STAGE;
+        run.tile<D>(kt, kt + TILE, plain, turned, q, first + AT_STAGE > fewest ? sees - first - 4 * half : AT_STAGE, A.s.scale2, o);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // (the stage has been read)
+        fill(t + 2);
+    }
+    wait_dma<0>();
+    run.sum = sl_both_sum(run.sum);
+    __syncthreads();
+    float *room = reinterpret_cast<float *>(lds), *stats = room + 4 * BLOCKS * 1024;
+#pragma unroll
+    for (int m = 0; m < BLOCKS; ++m) sl_leave_block(room + (wave * BLOCKS + m) * 1024, lane, o[m]);
+    if (half == 0) stats[wave * 64 + lane] = run.top, stats[wave * 64 + 32 + lane] = run.sum;
+    __syncthreads();
+    float top[4], sum = 0.0f, most = -INFINITY;
+    sl_f4 by;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top[w] = stats[w * 64 + (lane & 31)], most = fmaxf(most, top[w]);
+    const float ref = most == -INFINITY ? 0.0f : most;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        by[w] = __builtin_amdgcn_exp2f(top[w] - ref);
+        sum = fmaf(stats[w * 64 + 32 + (lane & 31)], by[w], sum);
+    }
+    const bool there = row < at.count;
+    const float whole = sum == 0.0f ? 0.0f : 1.0f / sum;
+    unsigned char *out = A.out.p + (long long)(at.first + mine) * A.out.token + head * A.out.head;
+    for (int m = wave; m < BLOCKS; m += 4) sl_put_block(out, there, half, A.s.octets, sl_four_blocks(room + m * 1024, BLOCKS * 1024, lane, by), m, whole);
+    if (A.lse && there && wave == 0 && half == 0)
+        A.lse[(long long)head * A.s.tokens_q + at.first + mine] = sum == 0.0f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * LN2;
+}
+
 // ---- backward ----
 
 // dq: queries to lanes as in the forward pass; S and dP of 32 keys at a time.  It also leaves what the pass over keys needs of a query.
@@ -147,6 +223,7 @@ __global__ void __launch_bounds__(256, 2) k_back_q(BackArgs A)
     extern __shared__ __align__(16) unsigned char lds[];
     constexpr int TILE = AT_TILE * 2 * D, STEPS = D / 16, BLOCKS = D / 32;
     const SlItem item = sl_item(blockIdx.x, (unsigned)A.s.heads);
+    if (blockIdx.x == 0 && threadIdx.x < 2) A.stats[A.none + threadIdx.x] = threadIdx.x == 0 ? INFINITY : 0.0f;
     if (item.tile >= A.s.tiles) return;
     SlSpan at;
     if (!sl_find(A.s.q_start, A.s.n, A.s.tokens_q, AT_ROWS, A.s.tiles, item.tile, true, at)) return;
@@ -242,7 +319,6 @@ __global__ void __launch_bounds__(256, 2) k_back_q(BackArgs A)
             }
         }
     }
-    if (blockIdx.x == 0 && threadIdx.x < 2) A.stats[A.none + threadIdx.x] = threadIdx.x == 0 ? INFINITY : 0.0f;
     if (row < at.count && half == 0) {
         float *to = A.stats + (long long)head * A.s.tokens_q + token;
         to[0] = lse2;
@@ -251,10 +327,145 @@ __global__ void __launch_bounds__(256, 2) k_back_q(BackArgs A)
     sl_put_row<D>(A.dq.p + token * A.dq.token + head * A.dq.head, row < at.count, half, A.s.octets, dq, A.s.scale);
 }
 
+// Few tiles: 32 queries to a workgroup, whose four waves take every fourth 32 keys; see k_attend_few.
+template <int D>
+__global__ void __launch_bounds__(256, 1) k_back_q_few(BackArgs A)
+{
+    extern __shared__ __align__(16) unsigned char lds[];
+    __shared__ float sums[4][32];
+    constexpr int TILE = AT_STAGE * 2 * D, STEPS = D / 16, BLOCKS = D / 32, LOADS = 2 * SlWaveLoad<D>::LOADS;
+    const SlItem item = sl_item(blockIdx.x, (unsigned)A.s.heads);
+    if (blockIdx.x == 0 && threadIdx.x < 2) A.stats[A.none + threadIdx.x] = threadIdx.x == 0 ? INFINITY : 0.0f;
+    if (item.tile >= A.s.tiles) return;
+    SlSpan at;
+    if (!sl_find(A.s.q_start, A.s.n, A.s.tokens_q, 32, A.s.tiles, item.tile, true, at)) return;
+    int k0, kn;
+    sl_rows_of(A.s.k_start, A.s.k_count, at.s, A.s.tokens_k, k0, kn);
+    const int lane = threadIdx.x & 63, wave = sl_uniform((int)(threadIdx.x >> 6)), half = lane >> 5;
+    const int head = (int)item.head, kv = head / A.s.group, shift = kn - at.count;
+    const int row = at.row0 + (lane & 31), mine = min(row, at.count - 1);
+    const long long token = at.first + mine;
+    const unsigned char *k = A.k.p + (long long)k0 * A.k.token + kv * A.k.head, *v = A.v.p + (long long)k0 * A.v.token + kv * A.v.head;
+    SlWaveLoad<D> lk, lv;
+    lk.setup(lane, A.s.octets, A.k.token);
+    lv.setup(lane, A.s.octets, A.v.token);
+    unsigned char *own = lds + wave * (4 * TILE);
+    const unsigned lds0 = (unsigned)(unsigned long long)(__attribute__((address_space(3))) unsigned char *)own;
+    const int sees = A.s.causal ? min(kn, mine + shift + 1) : kn;
+    const int all = A.s.causal ? min(kn, min(at.row0 + 31, at.count - 1) + shift + 1) : kn;
+    const int tiles = (max(all, 0) + AT_STAGE - 1) / AT_STAGE, steps = tiles > wave ? (tiles - wave + 3) / 4 : 0;
+    const bool few = (A.s.causal ? min(kn, at.row0 + shift + 1) : kn) <= FEW_KEYS;
+    const int total = few ? 2 * steps : steps;
+    auto fill = [&](int i) __attribute__((always_inline)) {
+        const int from = (wave + 4 * (min(i, total - 1) % steps)) * AT_STAGE;
+        const unsigned to = lds0 + (unsigned)(i & 1) * (2 * TILE);
+        lk.load(k, from, kn - from, to);
+        lv.load(v, from, kn - from, to + TILE);
+    };
+    if (steps > 0) fill(0), fill(1);
+    sl_b8 q[STEPS], g[STEPS];
+    sl_own_row<D>(A.dout.p + token * A.dout.token + head * A.dout.head, half, A.s.octets, g);
+    float delta = 0.0f;
+    {
+        sl_own_row<D>(A.out.p + token * A.out.token + head * A.out.head, half, A.s.octets, q);
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) delta = fmaf((float)q[i][e], (float)g[i][e], delta);
+        delta = sl_both_sum(delta);
+    }
+    sl_own_row<D>(A.q.p + token * A.q.token + head * A.q.head, half, A.s.octets, q);
+    const float lse = A.lse[(long long)head * A.s.tokens_q + token], lse2 = lse == -INFINITY ? 0.0f : lse * LOG2E;
+    const int plain = sl_plain_base<D>(lane), turned = sl_turned_base<D>(lane);
+    // P (dP - less) of step n
+    auto scores = [&](int n, float less) __attribute__((always_inline)) {
+        wait_dma<LOADS>();
+        const unsigned char *kt = own + (n & 1) * (2 * TILE), *vt = kt + TILE;
+        sl_f16 s = sl_zero16(), dp = sl_zero16();
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < STEPS; ++j) {
+            s = sl_mfma(sl_plain<D>(kt, plain, 0, j), q[j], s);
+            dp = sl_mfma(sl_plain<D>(vt, plain, 0, j), g[j], dp);
+        }
+        sl_reads_ahead<2 * STEPS, 8>();
+        __builtin_amdgcn_sched_barrier(0);
+        const int left = sees - (wave + 4 * (n % steps)) * AT_STAGE - 4 * half;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const float x = fmaf(s[e], A.s.scale2, -lse2);
+            s[e] = __builtin_amdgcn_exp2f(8 * (e >> 2) + (e & 3) < left ? x : -INFINITY) * (dp[e] - less);
+        }
+        return s;
+    };
+    auto again = [&](int n) __attribute__((always_inline)) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // (the stage has been read)
+        fill(n + 2);
+    };
+    int n = 0;
+    if (few) {
+        float sum = 0.0f;
+#pragma unroll 1
+        for (; n < steps; ++n) {
+            const sl_f16 s = scores(n, 0.0f);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sum = sum + s[e];
+            again(n);
+        }
+        sum = sl_both_sum(sum);
+        if (half == 0) sums[wave][lane] = sum;
+        __syncthreads();
+        delta = ((sums[0][lane & 31] + sums[1][lane & 31]) + sums[2][lane & 31]) + sums[3][lane & 31];
+    }
+    sl_f16 dq[BLOCKS];
+#pragma unroll
+    for (int m = 0; m < BLOCKS; ++m) dq[m] = sl_zero16();
+#pragma unroll 1
+    for (; n < total; ++n) {
+        const sl_f16 s = scores(n, delta);
+        const unsigned char *kt = own + (n & 1) * (2 * TILE);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const sl_b8 ds = sl_operand(s, j);
+#pragma unroll
+            for (int m = 0; m < BLOCKS; ++m) dq[m] = sl_mfma(sl_turned<D>(kt, turned, m, j), ds, dq[m]);
+        }
+        again(n);
+    }
+    wait_dma<0>();
+    __syncthreads();
+    float *room = reinterpret_cast<float *>(lds);
+#pragma unroll
+    for (int m = 0; m < BLOCKS; ++m) sl_leave_block(room + (wave * BLOCKS + m) * 1024, lane, dq[m]);
+    __syncthreads();
+    for (int m = wave; m < BLOCKS; m += 4)
+        sl_put_block(A.dq.p + token * A.dq.token + head * A.dq.head, row < at.count, half, A.s.octets,
+                     sl_four_blocks(room + m * 1024, BLOCKS * 1024, lane, sl_f4{1.0f, 1.0f, 1.0f, 1.0f}), m, A.s.scale);
+    if (row < at.count && wave == 0 && half == 0) {
+        float *to = A.stats + (long long)head * A.s.tokens_q + token;
+        to[0] = lse2;
+        to[(long long)A.s.heads * A.s.tokens_q] = delta;
+    }
+}
+
+// Scores and dP of 32 queries (rows 8 j + e of a lane) into P and dS; queries before row `from` do not see the lane's key.
+SL_DEV void back_scores(sl_f16 &s, sl_f16 &dp, const float *stats, int from, float scale2)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const sl_f4 lse = *reinterpret_cast<const sl_f4 *>(stats + 8 * j), delta = *reinterpret_cast<const sl_f4 *>(stats + 32 + 8 * j);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float x = fmaf(s[4 * j + e], scale2, -lse[e]);
+            s[4 * j + e] = __builtin_amdgcn_exp2f(8 * j + e < from ? -INFINITY : x);
+            dp[4 * j + e] = s[4 * j + e] * (dp[4 * j + e] - delta[e]);
+        }
+    }
+}
+
 // dk and dv: 128 keys of one key head, 32 to a wave, over all queries of the heads that share it, 32 at a time; the sums over the heads are
 // made in registers, in their order.  A wave holds its keys in registers and its values in LDS, so that two workgroups fit a compute unit
 // and one's exponentials run beside the other's products.
-enum { AT_STAGE = 32 };
 template <int D>
 __global__ void __launch_bounds__(256, 2) k_back_kv(BackArgs A)
 {
@@ -341,18 +552,7 @@ __global__ void __launch_bounds__(256, 2) k_back_kv(BackArgs A)
             __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
-        const int from = key_first - tile - 4 * half;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const sl_f4 lse = *reinterpret_cast<const sl_f4 *>(stats + 8 * j), delta = *reinterpret_cast<const sl_f4 *>(stats + 32 + 8 * j);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                // (a query that does not see the key: exp(-infinity))
-                const float x = fmaf(s[4 * j + e], A.s.scale2, -lse[e]);
-                s[4 * j + e] = __builtin_amdgcn_exp2f(8 * j + e < from ? -INFINITY : x);
-                dp[4 * j + e] = s[4 * j + e] * (dp[4 * j + e] - delta[e]);
-            }
-        }
+        back_scores(s, dp, stats, key_first - tile - 4 * half, A.s.scale2);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -375,6 +575,95 @@ __global__ void __launch_bounds__(256, 2) k_back_kv(BackArgs A)
     sl_put_row<D>(A.dv.p + token * A.dv.token + kv * A.dv.head, key < kn, half, A.s.octets, dv, 1.0f);
 }
 
+// Few tiles: 32 keys to a workgroup, whose four waves take every fourth 32 queries (of the heads that share the keys, one head after the
+// other), in LDS of their own, and wait for nobody; their sums meet at the end.
+template <int D>
+__global__ void __launch_bounds__(256, 1) k_back_kv_few(BackArgs A)
+{
+    extern __shared__ __align__(16) unsigned char lds[];
+    constexpr int TILE = AT_STAGE * 2 * D, STAGE = 2 * TILE + 256, STEPS = D / 16, BLOCKS = D / 32, LOADS = 2 * SlWaveLoad<D>::LOADS + 1;
+    const int kv_heads = A.s.heads / A.s.group;
+    const SlItem item = sl_item(blockIdx.x, (unsigned)kv_heads);
+    if (item.tile >= A.s.tiles) return;
+    SlSpan at;
+    if (!sl_find(A.s.k_start, A.s.n, A.s.tokens_k, 32, A.s.tiles, item.tile, false, at)) return;
+    int q0, qn, k0, kn;
+    sl_rows_of(A.s.q_start, nullptr, at.s, A.s.tokens_q, q0, qn);
+    sl_rows_of(A.s.k_start, A.s.k_count, at.s, A.s.tokens_k, k0, kn);
+    if (at.row0 >= kn) return;
+    const int lane = threadIdx.x & 63, wave = sl_uniform((int)(threadIdx.x >> 6)), half = lane >> 5;
+    const int kv = (int)item.head, shift = kn - qn;
+    const int key = at.row0 + (lane & 31), mine = min(key, kn - 1);
+    const long long token = k0 + mine;
+    unsigned char *own = lds + wave * (2 * STAGE);
+    const unsigned lds0 = (unsigned)(unsigned long long)(__attribute__((address_space(3))) unsigned char *)own;
+    SlWaveLoad<D> lq, lg;
+    lq.setup(lane, A.s.octets, A.q.token);
+    lg.setup(lane, A.s.octets, A.dout.token);
+    const int first = A.s.causal ? max(at.row0 - shift, 0) / AT_STAGE : 0, tiles = (qn + AT_STAGE - 1) / AT_STAGE;
+    const int key_first = A.s.causal ? key - shift : 0;
+    const int per_head = max(tiles - first, 0), stages = per_head * A.s.group, steps = stages > wave ? (stages - wave + 3) / 4 : 0;
+    auto fill = [&](int n) __attribute__((always_inline)) {
+        const int i = wave + 4 * min(n, steps - 1), head = kv * A.s.group + i / per_head, tile = (first + i % per_head) * AT_STAGE;
+        const unsigned to = lds0 + (unsigned)(n & 1) * STAGE;
+        lq.load(A.q.p + (long long)q0 * A.q.token + head * A.q.head, tile, qn - tile, to);
+        lg.load(A.dout.p + (long long)q0 * A.dout.token + head * A.dout.head, tile, qn - tile, to + TILE);
+        const int row = tile + (lane & 31);
+        const float *stats = A.stats + ((long long)half * A.s.heads + head) * A.s.tokens_q + q0 + row;
+        dma4(row < qn ? stats : A.stats + A.none + half, to + 2 * TILE);
+    };
+    if (steps > 0) fill(0), fill(1);
+    sl_b8 k[STEPS], v[STEPS];
+    sl_own_row<D>(A.k.p + token * A.k.token + kv * A.k.head, half, A.s.octets, k);
+    sl_own_row<D>(A.v.p + token * A.v.token + kv * A.v.head, half, A.s.octets, v);
+    const int plain = sl_plain_base<D>(lane), turned = sl_turned_base<D>(lane);
+    sl_f16 dk[BLOCKS], dv[BLOCKS];
+#pragma unroll
+    for (int m = 0; m < BLOCKS; ++m) dk[m] = dv[m] = sl_zero16();
+#pragma unroll 1
+    for (int n = 0; n < steps; ++n) {
+        wait_dma<LOADS>();
+        const int tile = (first + (wave + 4 * n) % per_head) * AT_STAGE;
+        const unsigned char *qt = own + (n & 1) * STAGE, *gt = qt + TILE;
+        const float *stats = reinterpret_cast<const float *>(qt + 2 * TILE) + 4 * half;
+        sl_f16 s = sl_zero16(), dp = sl_zero16();
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < STEPS; ++j) {
+            s = sl_mfma(sl_plain<D>(qt, plain, 0, j), k[j], s);
+            dp = sl_mfma(sl_plain<D>(gt, plain, 0, j), v[j], dp);
+        }
+        sl_reads_ahead<2 * STEPS, 8>();
+        __builtin_amdgcn_sched_barrier(0);
+        back_scores(s, dp, stats, key_first - tile - 4 * half, A.s.scale2);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const sl_b8 p = sl_operand(s, j), ds = sl_operand(dp, j);
+#pragma unroll
+            for (int m = 0; m < BLOCKS; ++m) {
+                dv[m] = sl_mfma(sl_turned<D>(gt, turned, m, j), p, dv[m]);
+                dk[m] = sl_mfma(sl_turned<D>(qt, turned, m, j), ds, dk[m]);
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // (the stage has been read)
+        fill(n + 2);
+    }
+    wait_dma<0>();
+    __syncthreads();
+    float *room = reinterpret_cast<float *>(lds);
+#pragma unroll
+    for (int m = 0; m < BLOCKS; ++m) {
+        sl_leave_block(room + (wave * 2 * BLOCKS + m) * 1024, lane, dk[m]);
+        sl_leave_block(room + (wave * 2 * BLOCKS + BLOCKS + m) * 1024, lane, dv[m]);
+    }
+    __syncthreads();
+    for (int i = wave; i < 2 * BLOCKS; i += 4) {
+        const sl_f16 x = sl_four_blocks(room + i * 1024, 2 * BLOCKS * 1024, lane, sl_f4{1.0f, 1.0f, 1.0f, 1.0f});
+        if (i < BLOCKS) sl_put_block(A.dk.p + token * A.dk.token + kv * A.dk.head, key < kn, half, A.s.octets, x, i, A.s.scale);
+        else sl_put_block(A.dv.p + token * A.dv.token + kv * A.dv.head, key < kn, half, A.s.octets, x, i - BLOCKS, 1.0f);
+    }
+}
+
 int check_launch()
 {
     const hipError_t err = hipGetLastError();
@@ -382,6 +671,18 @@ int check_launch()
     sl_note_hip_error(err);
     return SL_ERR_HIP;
 }
+
+// 32 rows to a workgroup, which splits the other side among its waves, or 128.  With W workgroups of 128 rows that each walk a mean of `walk`
+// rows, these all run at once below two to a compute unit, and take as long as the longest walk; the others take a quarter of the walk each,
+// four times as many of them, one (heads up to 64: two) to a compute unit, and a start of about 4 us every time.  So the limit
+// rises with the walk to 400 (900), and is 64 (128) where four times as many still run at once.  Forward, us, 32 rows / 128, 16 heads of 128: 2 x 1024 tokens (W = 288) 37 / 26, 2048 (272) 48 / 44, 4 heads, 8192 (260)
+// 125 / 178; 16 heads of 64: 4 x 1024 (576) 32 / 22, 2048 (272) 25 / 36, 4096 (528) 67 / 69; keys and values, 4 heads of 64 for 16, 9 sequences up to 1021 (160) 46 / 151.
+bool few_tiles(int64_t rows, int64_t n, int64_t heads, int64_t other, int64_t times, bool narrow)
+{
+    const int64_t w = (rows / AT_ROWS + n) * heads, walk = other / n * times;
+    return w <= (narrow ? 128 : 64) || w * (walk + 1400) < (narrow ? 900 : 400) * walk;
+}
+unsigned tile_count(int64_t tokens, int64_t n, bool few) { return (unsigned)(tokens / (few ? 32 : AT_ROWS) + n); }
 
 template <class Args>
 int launch(void (*k)(Args), const Args &A, long long heads, unsigned lds, hipStream_t st)
@@ -412,10 +713,12 @@ int sl_attention(const sl_attention_shape *shape, const sl_heads *q, const sl_he
         return SL_ERR_INVALID_ARG;
     if (out->data == q->data || (keys && (out->data == k->data || out->data == v->data)) || out->data == (void *)lse) return SL_ERR_INVALID_ARG;
     A.lse = lse;
-    A.s.tiles = (unsigned)A.s.tokens_q / AT_ROWS + (unsigned)A.s.n;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (A.s.octets <= 8) return launch(k_attend<64>, A, A.s.heads, 4 * AT_TILE * 2 * 64, st);
-    return launch(k_attend<128>, A, A.s.heads, 4 * AT_TILE * 2 * 128, st);
+    const bool narrow = A.s.octets <= 8, few = few_tiles(A.s.tokens_q, A.s.n, A.s.heads, A.s.tokens_k, 1, narrow);
+    const unsigned tile = AT_TILE * 2 * (narrow ? 64 : 128);
+    A.s.tiles = tile_count(A.s.tokens_q, A.s.n, few);
+    if (few) return launch(narrow ? k_attend_few<64> : k_attend_few<128>, A, A.s.heads, 8 * tile, st);
+    return launch(narrow ? k_attend<64> : k_attend<128>, A, A.s.heads, 4 * tile, st);
 }
 
 size_t sl_attention_workspace_bytes(int64_t tokens_q, int64_t heads)
@@ -448,12 +751,17 @@ int sl_attention_backward(const sl_attention_shape *shape, const sl_heads *q, co
     const bool narrow = A.s.octets <= 8;
     const unsigned tile = AT_TILE * 2 * (narrow ? 64 : 128);
     if (queries) {
-        A.s.tiles = (unsigned)A.s.tokens_q / AT_ROWS + (unsigned)A.s.n;
-        if (const int rc = launch(narrow ? k_back_q<64> : k_back_q<128>, A, A.s.heads, 4 * tile, st)) return rc;
+        const bool few = few_tiles(A.s.tokens_q, A.s.n, A.s.heads, A.s.tokens_k, 1, narrow);
+        A.s.tiles = tile_count(A.s.tokens_q, A.s.n, few);
+        if (const int rc = few ? launch(narrow ? k_back_q_few<64> : k_back_q_few<128>, A, A.s.heads, 8 * tile, st)
+                               : launch(narrow ? k_back_q<64> : k_back_q<128>, A, A.s.heads, 4 * tile, st))
+            return rc;
     }
     if (!keys) return SL_OK;
-    A.s.tiles = (unsigned)A.s.tokens_k / AT_ROWS + (unsigned)A.s.n;
-    return launch(narrow ? k_back_kv<64> : k_back_kv<128>, A, A.s.heads / A.s.group, 4 * tile + 512, st);
+    const bool few = few_tiles(A.s.tokens_k, A.s.n, kv_heads, A.s.tokens_q, A.s.group, narrow);
+    A.s.tiles = tile_count(A.s.tokens_k, A.s.n, few);
+    if (few) return launch(narrow ? k_back_kv_few<64> : k_back_kv_few<128>, A, kv_heads, 8 * tile + 2048, st);
+    return launch(narrow ? k_back_kv<64> : k_back_kv<128>, A, kv_heads, 4 * tile + 512, st);
 }
 
 }  // extern "C"

@@ -6,7 +6,7 @@
 namespace {
 
 // Keys of a workgroup, and how many a wave takes at a time.
-enum { LEAST_PART = 128, KEYS = 32, MOST_GROUPS = 1280, LONGEST_PART = 2048 };
+enum { LEAST_PART = 128, KEYS = AT_STAGE, MOST_GROUPS = 1280, LONGEST_PART = 2048 };
 
 struct TokenArgs {
     SlSequences s;
@@ -16,37 +16,6 @@ struct TokenArgs {
     unsigned part;               // keys in a part
 };
 
-// 32 rows of a cache to a wave's own LDS.
-template <int D>
-struct WaveLoad {
-    enum { PIECES = D / 8, PER = 64 / PIECES, LOADS = KEYS / PER };
-    unsigned at[LOADS], off[LOADS];
-    int row;
-    long long token;
-
-    SL_DEV void setup(int lane, int octets, long long stride)
-    {
-        row = lane / PIECES, token = stride;
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            at[i] = (unsigned)min((lane % PIECES) ^ sl_turn<D>(row + i * PER), octets - 1) * 16u;
-            off[i] = (unsigned)(row + i * PER) * (unsigned)token + at[i];
-        }
-    }
-    // rows first .. + 31, of which `count` exist (at least one)
-    SL_DEV void load(const unsigned char *base, int first, int count, unsigned lds) const
-    {
-        const unsigned char *from = base + first * token;
-        if (count >= KEYS) {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) dma16(from, off[i], lds + i * 1024u);
-        } else {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) dma16(from, (unsigned)min(row + i * PER, count - 1) * (unsigned)token + at[i], lds + i * 1024u);
-        }
-    }
-};
-
 // A part of a sequence's keys for up to 32 heads that share a key head: the heads are the columns of the score tile.  Every wave takes every
 // fourth 32 keys of the part, in two stages of LDS of its own, and waits for nobody; the waves' results meet at the end.  Bound by the cache's
 // bytes: each is read once, and the matrix unit idles.
@@ -54,7 +23,7 @@ template <int D>
 __global__ void __launch_bounds__(256, 1) k_token(TokenArgs A, unsigned blocks)
 {
     extern __shared__ __align__(16) unsigned char lds[];
-    constexpr int TILE = KEYS * 2 * D, STEPS = D / 16, BLOCKS = D / 32, LOADS = 2 * WaveLoad<D>::LOADS;
+    constexpr int TILE = KEYS * 2 * D, STEPS = D / 16, BLOCKS = D / 32, LOADS = 2 * SlWaveLoad<D>::LOADS;
     const unsigned kv_heads = (unsigned)(A.s.heads / A.s.group);
     const SlItem item = sl_item(blockIdx.x, kv_heads * blocks);
     if (item.tile >= A.s.tiles) return;
@@ -69,7 +38,7 @@ __global__ void __launch_bounds__(256, 1) k_token(TokenArgs A, unsigned blocks)
     sl_own_row<D>(A.q.p + at.s * A.q.token + head * A.q.head, half, A.s.octets, q);
     const long long k0 = (long long)at.first + at.row0;
     const unsigned char *k = A.k.p + k0 * A.k.token + kv * A.k.head, *v = A.v.p + k0 * A.v.token + kv * A.v.head;
-    WaveLoad<D> lk, lv;
+    SlWaveLoad<D> lk, lv;
     lk.setup(lane, A.s.octets, A.k.token);
     lv.setup(lane, A.s.octets, A.v.token);
     unsigned char *mine = lds + wave * (4 * TILE);
@@ -78,7 +47,7 @@ __global__ void __launch_bounds__(256, 1) k_token(TokenArgs A, unsigned blocks)
     sl_f16 o[BLOCKS];
 #pragma unroll
     for (int m = 0; m < BLOCKS; ++m) o[m] = sl_zero16();
-    float top = -INFINITY, ref = 0.0f, sum = 0.0f;
+    SlRunning run;
     const int tiles = (n + KEYS - 1) / KEYS, steps = tiles > wave ? (tiles - wave + 3) / 4 : 0;
     // (past the last step it brings that one again, so that every step waits for the same number of loads)
     auto fill = [&](int i) __attribute__((always_inline)) {
@@ -91,44 +60,13 @@ __global__ void __launch_bounds__(256, 1) k_token(TokenArgs A, unsigned blocks)
 #pragma unroll 1
     for (int t = 0; t < steps; ++t) {
         wait_dma<LOADS>();
-        const unsigned char *kt = mine + (t & 1) * (2 * TILE), *vt = kt + TILE;
-        sl_f16 s = sl_zero16();
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i) s = sl_mfma(sl_plain<D>(kt, plain, 0, i), q[i], s);
-        const int left = n - (wave + 4 * t) * KEYS - 4 * half;
-        if (left < KEYS) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-                if (8 * (e >> 2) + (e & 3) >= left) s[e] = -INFINITY;
-        }
-        float now = s[0];
-#pragma unroll
-        for (int e = 1; e < 16; ++e) now = fmaxf(now, s[e]);
-        now = sl_both_max(now) * A.s.scale2;
-        if (sl_ballot(now > top + 8.0f)) {
-            const float next = fmaxf(top, now), to = next == -INFINITY ? 0.0f : next, by = __builtin_amdgcn_exp2f(top - to);
-            top = next, ref = to, sum = sum * by;
-#pragma unroll
-            for (int m = 0; m < BLOCKS; ++m)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) o[m][e] = o[m][e] * by;
-        }
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], A.s.scale2, -ref));
-            sum = sum + s[e];
-        }
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            const sl_b8 p = sl_operand(s, g);
-#pragma unroll
-            for (int m = 0; m < BLOCKS; ++m) o[m] = sl_mfma(sl_turned<D>(vt, turned, m, g), p, o[m]);
-        }
+        const unsigned char *kt = mine + (t & 1) * (2 * TILE);
+        run.tile<D>(kt, kt + TILE, plain, turned, q, min(n - (wave + 4 * t) * KEYS, (int)KEYS) - 4 * half, A.s.scale2, o);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // (the stage has been read)
         fill(t + 2);
     }
     wait_dma<0>();
-    sum = sl_both_sum(sum);
+    run.sum = sl_both_sum(run.sum);
     __syncthreads();
     // the waves' sums through LDS: column after column, a pad of one between them
     float *all = reinterpret_cast<float *>(lds);
@@ -138,7 +76,7 @@ __global__ void __launch_bounds__(256, 1) k_token(TokenArgs A, unsigned blocks)
     for (int m = 0; m < BLOCKS; ++m)
 #pragma unroll
         for (int e = 0; e < 16; ++e) all[(wave * 32 + (lane & 31)) * PITCH + 32 * m + 8 * (e >> 2) + 4 * half + (e & 3)] = o[m][e];
-    if (half == 0) stats[(wave * 32 + lane) * 2] = top, stats[(wave * 32 + lane) * 2 + 1] = sum;
+    if (half == 0) stats[(wave * 32 + lane) * 2] = run.top, stats[(wave * 32 + lane) * 2 + 1] = run.sum;
     __syncthreads();
     const int heads_here = min(A.s.group - first_head, 32), dim = A.s.octets * 8;
     for (int i = threadIdx.x; i < heads_here * dim; i += 256) {

@@ -29,7 +29,7 @@ struct LossArgs {
 SL_DEV float wave_max(float v)
 {
 #pragma unroll
-    for (int l = 0; l < 6; ++l) v = fmaxf(v, __int_as_float(sl_partner(__float_as_int(v), l)));
+    for (int l = 0; l < 6; ++l) v = __builtin_elementwise_maximum(v, __int_as_float(sl_partner(__float_as_int(v), l)));
     return v;
 }
 
@@ -41,7 +41,7 @@ SL_DEV float all_max(float v, float *room, int wave, int lane)
         if (lane == 0) room[wave] = v;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < WAVES; ++i) v = fmaxf(v, room[i]);
+        for (int i = 0; i < WAVES; ++i) v = __builtin_elementwise_maximum(v, room[i]);
     }
     return v;
 }
@@ -65,19 +65,20 @@ SL_DEV void token_loss(const LossArgs &A, long long row, double logp, double &lo
     }
 }
 
+// Eight elements of a row from `col` on, of which `from` .. n - 1 exist (the row does not reach further, or begins inside them).
 template <bool B16>
-SL_DEV void put_octet(const LossArgs &A, long long at, int n, const float (&v)[8])
+SL_DEV void put_octet(const LossArgs &A, long long at, int from, int n, const float (&v)[8])
 {
     if constexpr (B16) {
         typedef unsigned u4a __attribute__((ext_vector_type(4), aligned(2)));
         unsigned short *o = static_cast<unsigned short *>(A.dlogits) + at;
-        if (n >= 8) {
+        if (from <= 0 && n >= 8) {
             __builtin_nontemporal_store(u4a{sl_bf16_pair(v[0], v[1]), sl_bf16_pair(v[2], v[3]), sl_bf16_pair(v[4], v[5]), sl_bf16_pair(v[6], v[7])},
                                         reinterpret_cast<u4a *>(o));
         } else {
 #pragma unroll
-            for (int i = 0; i < 7; ++i)
-                if (i < n) o[i] = (unsigned short)sl_bf16_bits(v[i]);
+            for (int i = 0; i < 8; ++i)
+                if (i >= from && i < n) o[i] = (unsigned short)sl_bf16_bits(v[i]);
         }
     } else {
         typedef float f4a __attribute__((ext_vector_type(4), aligned(4)));
@@ -98,48 +99,64 @@ template <bool B16>
 SL_DEV void load_octet(const LossArgs &A, long long row, long long col, SlOctet<B16> &v)
 {
     const int n = (int)max(min(A.vocab - col, 8ll), 0ll);
-    v.load(A.logits, row * A.ld + col, n);
-    if (n < 8) {
+    if constexpr (B16) {
+        if (col >= 0 && n >= 8) {
+            v.load(A.logits, row * A.ld + col, 8);
+        } else {
+            const unsigned short *p = static_cast<const unsigned short *>(A.logits) + (row * A.ld + col);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if constexpr (B16) {
-                if (i >= n) v.w[i >> 1] |= 0xFF80u << (16 * (i & 1));
-            } else {
+            for (int i = 0; i < 4; ++i) v.w[i] = 0xFF80FF80u;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (col + i >= 0 && i < n) v.w[i >> 1] = (v.w[i >> 1] & (i & 1 ? 0xFFFFu : 0xFFFF0000u)) | (unsigned)p[i] << (16 * (i & 1));
+        }
+    } else {
+        v.load(A.logits, row * A.ld + col, n);
+        if (n < 8) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
                 if (i >= n) v.w[i] = 0xFF800000u;
-            }
         }
     }
 }
 
+// (a NaN makes the largest one, and with it everything of the row)
 template <bool B16>
 SL_DEV float octet_max(const SlOctet<B16> &v, float m)
 {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = fmaxf(m, v.value(i));
+    for (int i = 0; i < 8; ++i) m = __builtin_elementwise_maximum(m, v.value(i));
     return m;
 }
 
 SL_DEV float exp_at(float z, float m) { return __builtin_amdgcn_exp2f((z - m) * LOG2E); }
 
-// One row to a workgroup of WAVES waves, OCT times eight logits in a lane.
+// One row to a team of WAVES waves, OCT times eight logits in a lane.  The exponentials take the logits' place in the registers: the
+// gradient is them times the row's share, and half of the arithmetic is exponentials.  Teams are as small as the registers allow, several to
+// a compute unit: one reads while another writes.  (8192 x 50,257 bf16: exponentials made twice, 16 waves, one team 436 us.)
+// Rows of bf16 that begin inside 16 bytes are taken from the 16 bytes' begin on (rows of 50,257: 428 us without, 353 with aligned ones).
 // (LONG: a vocabulary that does not fit the registers is read twice)
 template <bool B16, int WAVES, int OCT, bool LONG>
-__global__ void __launch_bounds__(64 * WAVES) k_token_loss(LossArgs A)
+__global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, OCT == 13 ? 4 : 1) k_token_loss(LossArgs A)
 {
     __shared__ float tops[WAVES];
     __shared__ double sums[WAVES];
     __shared__ float told[2];
     constexpr long long STEP = WAVES * OCT * 512;
-    const int lane = threadIdx.x & 63, wave = sl_uniform((int)(threadIdx.x >> 6));
-    const long long row = blockIdx.x, target = A.targets[row];
+    const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : sl_uniform((int)(threadIdx.x >> 6));
+    const long long row = WAVES == 1 ? blockIdx.x * 4ll + sl_uniform((int)(threadIdx.x >> 6)) : blockIdx.x;
+    if (row >= A.rows) return;                    // (one wave to a row: no barrier follows)
+    const bool leader = wave == 0 && lane == 0;
+    const long long target = A.targets[row];
     const float weight = A.weights ? A.weights[row] : 1.0f;
     const bool there = target >= 0 && target < A.vocab, counts = there && weight != 0.0f;
-    if (!counts && threadIdx.x == 0) {
+    if (!counts && leader) {
         if (A.each) A.each[row] = 0.0;
         if (!there && A.logp) A.logp[row] = 0.0f;
     }
+    const int pre = B16 ? (int)(((unsigned long long)A.logits >> 1) + (unsigned long long)(row * A.ld)) & 7 : 0;     // elements in front of the row
     float slope = 0.0f, share = 0.0f, m = 0.0f;
-    SlOctet<B16> v[OCT];
+    float e[OCT][8];
     if (counts || (there && A.logp)) {
         m = -INFINITY;
         double sum = 0.0;
@@ -147,13 +164,14 @@ __global__ void __launch_bounds__(64 * WAVES) k_token_loss(LossArgs A)
                              : static_cast<const float *>(A.logits)[row * A.ld + target];
         if constexpr (LONG) {
             float mine = -INFINITY, part = 0.0f;
-            for (long long base = 0; base < A.vocab; base += STEP) {
+            for (long long base = 0; base < A.vocab + pre; base += STEP) {
+                SlOctet<B16> v[OCT];
 #pragma unroll
-                for (int j = 0; j < OCT; ++j) load_octet(A, row, base + ((j * WAVES + wave) * 64 + lane) * 8, v[j]);
+                for (int j = 0; j < OCT; ++j) load_octet(A, row, base + ((j * WAVES + wave) * 64 + lane) * 8 - pre, v[j]);
                 float now = mine;
 #pragma unroll
                 for (int j = 0; j < OCT; ++j) now = octet_max(v[j], now);
-                if (now > mine) part = part * exp_at(mine, now), mine = now;
+                if (now != mine) part = part * exp_at(mine, now), mine = now;
                 const float from = mine == -INFINITY ? 0.0f : mine;
 #pragma unroll
                 for (int j = 0; j < OCT; ++j)
@@ -163,8 +181,9 @@ __global__ void __launch_bounds__(64 * WAVES) k_token_loss(LossArgs A)
             m = all_max<WAVES>(mine, tops, wave, lane);
             sum = mine == -INFINITY ? (double)part : (double)part * (double)exp_at(mine, m);
         } else {
+            SlOctet<B16> v[OCT];
 #pragma unroll
-            for (int j = 0; j < OCT; ++j) load_octet(A, row, ((j * WAVES + wave) * 64 + lane) * 8, v[j]);
+            for (int j = 0; j < OCT; ++j) load_octet(A, row, ((j * WAVES + wave) * 64 + lane) * 8 - pre, v[j]);
 #pragma unroll
             for (int j = 0; j < OCT; ++j) m = octet_max(v[j], m);
             m = all_max<WAVES>(m, tops, wave, lane);
@@ -172,51 +191,70 @@ __global__ void __launch_bounds__(64 * WAVES) k_token_loss(LossArgs A)
 #pragma unroll
             for (int j = 0; j < OCT; ++j)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) part = part + exp_at(v[j].value(i), m);
+                for (int i = 0; i < 8; ++i) {
+                    e[j][i] = exp_at(v[j].value(i), m);
+                    part = part + e[j][i];
+                }
             sum = (double)part;
         }
         sum = sl_wave_tree(sum, 6);
-        if (lane == 0) sums[wave] = sum;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            sum = sums[0];
+        if constexpr (WAVES > 1) {
+            if (lane == 0) sums[wave] = sum;
+            __syncthreads();
+        }
+        if (leader) {
+            if constexpr (WAVES > 1) {
 #pragma unroll
-            for (int i = 1; i < WAVES; ++i) sum = sum + sums[i];
+                for (int i = 1; i < WAVES; ++i) sum = sum + sums[i];
+            }
             const double logp = ((double)zt - (double)m) - log(sum);
             if (A.logp) A.logp[row] = (float)logp;
             if (counts) {
                 double loss, d;
                 token_loss(A, row, logp, loss, d);
                 if (A.each) A.each[row] = (double)weight * loss;
-                told[0] = (float)((double)weight * d);
-                told[1] = (float)(-((double)weight * d) / sum);
+                slope = (float)((double)weight * d), share = (float)(-((double)weight * d) / sum);
+                if constexpr (WAVES > 1) told[0] = slope, told[1] = share;
             }
         }
         if (A.dlogits && counts) {
-            __syncthreads();
-            slope = told[0], share = told[1];
+            if constexpr (WAVES > 1) {
+                __syncthreads();
+                slope = told[0], share = told[1];
+            } else {
+                slope = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(slope)));
+                share = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(share)));
+            }
         }
     }
     if (!A.dlogits) return;
-    for (long long base = 0; base < (LONG ? A.vocab : 1); base += STEP)
+    for (long long base = 0; base < (LONG ? A.vocab + pre : 1); base += STEP)
 #pragma unroll
         for (int j = 0; j < OCT; ++j) {
-            const long long col = base + ((j * WAVES + wave) * 64 + lane) * 8;
+            const long long col = base + ((j * WAVES + wave) * 64 + lane) * 8 - pre;
             const int n = (int)max(min(A.vocab - col, 8ll), 0ll);
             float d[8];
             if (counts) {
-                if constexpr (LONG) load_octet(A, row, col, v[j]);
-                const int at = (int)min(max(target - col, -1ll), 8ll);
+                if constexpr (LONG) {
+                    SlOctet<B16> v;
+                    load_octet(A, row, col, v);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    d[i] = exp_at(v[j].value(i), m) * share;
-                    if (i == at) d[i] = d[i] + slope;
+                    for (int i = 0; i < 8; ++i) d[i] = exp_at(v.value(i), m) * share;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) d[i] = e[j][i] * share;
+                }
+                const long long at = target - col;
+                if (at >= 0 && at < 8) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (i == at) d[i] = d[i] + slope;
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) d[i] = 0.0f;
             }
-            if (n > 0) put_octet<B16>(A, row * A.ldd + col, n, d);
+            if (n > 0) put_octet<B16>(A, row * A.ldd + col, (int)max(-col, 0ll), n, d);
         }
 }
 
@@ -245,14 +283,16 @@ int check_launch()
 template <bool B16>
 void launch(const LossArgs &A, hipStream_t st)
 {
-    const dim3 grid((unsigned)A.rows);
-    const long long octets = (A.vocab + 7) / 8;
-    if (octets <= 256) hipLaunchKernelGGL((k_token_loss<B16, 1, 4, false>), grid, dim3(64), 0, st, A);
+    const dim3 grid((unsigned)A.rows), four((unsigned)((A.rows + 3) / 4));
+    const bool aligned = !B16 || (((uintptr_t)A.logits & 15) == 0 && A.ld % 8 == 0);
+    const long long octets = (A.vocab + (aligned ? 7 : 14)) / 8;
+    if (octets <= 64) hipLaunchKernelGGL((k_token_loss<B16, 1, 1, false>), four, dim3(256), 0, st, A);
+    else if (octets <= 128) hipLaunchKernelGGL((k_token_loss<B16, 1, 2, false>), four, dim3(256), 0, st, A);
+    else if (octets <= 256) hipLaunchKernelGGL((k_token_loss<B16, 1, 4, false>), four, dim3(256), 0, st, A);
     else if (octets <= 1024) hipLaunchKernelGGL((k_token_loss<B16, 4, 4, false>), grid, dim3(256), 0, st, A);
-    else if (octets <= 2048) hipLaunchKernelGGL((k_token_loss<B16, 16, 2, false>), grid, dim3(1024), 0, st, A);
-    else if (octets <= 4096) hipLaunchKernelGGL((k_token_loss<B16, 16, 4, false>), grid, dim3(1024), 0, st, A);
-    else if (octets <= 6144) hipLaunchKernelGGL((k_token_loss<B16, 16, 6, false>), grid, dim3(1024), 0, st, A);
-    else if (octets <= 7168) hipLaunchKernelGGL((k_token_loss<B16, 16, 7, false>), grid, dim3(1024), 0, st, A);
+    else if (octets <= 2048) hipLaunchKernelGGL((k_token_loss<B16, 4, 8, false>), grid, dim3(256), 0, st, A);
+    else if (octets <= 4096) hipLaunchKernelGGL((k_token_loss<B16, 8, 8, false>), grid, dim3(512), 0, st, A);
+    else if (octets <= 6656) hipLaunchKernelGGL((k_token_loss<B16, 8, 13, false>), grid, dim3(512), 0, st, A);
     else if (octets <= 8192) hipLaunchKernelGGL((k_token_loss<B16, 16, 8, false>), grid, dim3(1024), 0, st, A);
     else hipLaunchKernelGGL((k_token_loss<B16, 16, 4, true>), grid, dim3(1024), 0, st, A);
 }
