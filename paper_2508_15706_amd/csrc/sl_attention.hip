@@ -687,10 +687,12 @@ unsigned tile_count(int64_t tokens, int64_t n, bool few) { return (unsigned)(tok
 template <class Args>
 int launch(void (*k)(Args), const Args &A, long long heads, unsigned lds, hipStream_t st)
 {
-    const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    if (err != hipSuccess) {
-        sl_note_hip_error(err);
-        return SL_ERR_HIP;
+    if (lds > 65536) {
+        const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (err != hipSuccess) {
+            sl_note_hip_error(err);
+            return SL_ERR_HIP;
+        }
     }
     hipLaunchKernelGGL(k, dim3(sl_item_groups(A.s.tiles, heads)), dim3(256), lds, st, A);
     return check_launch();

@@ -5,8 +5,8 @@
 
 namespace {
 
-// Keys of a workgroup, and how many a wave takes at a time.
-enum { LEAST_PART = 128, KEYS = AT_STAGE, MOST_GROUPS = 1280, LONGEST_PART = 2048 };
+// Keys of a part: one wave's work.
+enum { LEAST_PART = 32, LONGEST_PART = 512, MOST_WAVES = 1280 };
 
 struct TokenArgs {
     SlSequences s;
@@ -16,14 +16,15 @@ struct TokenArgs {
     unsigned part;               // keys in a part
 };
 
-// A part of a sequence's keys for up to 32 heads that share a key head: the heads are the columns of the score tile.  Every wave takes every
-// fourth 32 keys of the part, in two stages of LDS of its own, and waits for nobody; the waves' results meet at the end.  Bound by the cache's
-// bytes: each is read once, and the matrix unit idles.
+// A part of a sequence's keys for up to 32 heads that share a key head: the heads are the columns of the score tile.  One wave does it, 32
+// keys at a time, in two stages of LDS, and waits for nobody: five of them fit a compute unit, so that one's start and end lie beside
+// the others' loads.  Bound by the cache's bytes; the matrix unit idles.  (64 sequences, up to 16,384 keys, 5 heads of 128 - 596 MB: four waves to a
+// part of 2048 keys 122 us, of 512 183.)
 template <int D>
-__global__ void __launch_bounds__(256, 1) k_token(TokenArgs A, unsigned blocks)
+__global__ void __launch_bounds__(64, 2) k_token(TokenArgs A, unsigned blocks)
 {
     extern __shared__ __align__(16) unsigned char lds[];
-    constexpr int TILE = KEYS * 2 * D, STEPS = D / 16, BLOCKS = D / 32, LOADS = 2 * SlWaveLoad<D>::LOADS;
+    constexpr int TILE = AT_STAGE * 2 * D, STEPS = D / 16, BLOCKS = D / 32, LOADS = 2 * SlWaveLoad<D>::LOADS;
     const unsigned kv_heads = (unsigned)(A.s.heads / A.s.group);
     const SlItem item = sl_item(blockIdx.x, kv_heads * blocks);
     if (item.tile >= A.s.tiles) return;
@@ -31,94 +32,98 @@ __global__ void __launch_bounds__(256, 1) k_token(TokenArgs A, unsigned blocks)
     if (!sl_find_tile(A.s.k_start, A.s.n, A.s.tokens_k, A.part, item.tile, at)) return;
     const int kn = A.s.k_count ? min(max(A.s.k_count[at.s], 0), at.count) : at.count, n = min((int)A.part, kn - at.row0);
     if (n <= 0) return;
-    const int lane = threadIdx.x & 63, wave = sl_uniform((int)(threadIdx.x >> 6)), half = lane >> 5;
+    const int lane = threadIdx.x, half = lane >> 5;
     const int kv = (int)(item.head / blocks), first_head = (int)(item.head % blocks) * 32, in_group = first_head + (lane & 31);
     const int head = kv * A.s.group + min(in_group, A.s.group - 1);
-    sl_b8 q[STEPS];
-    sl_own_row<D>(A.q.p + at.s * A.q.token + head * A.q.head, half, A.s.octets, q);
     const long long k0 = (long long)at.first + at.row0;
     const unsigned char *k = A.k.p + k0 * A.k.token + kv * A.k.head, *v = A.v.p + k0 * A.v.token + kv * A.v.head;
     SlWaveLoad<D> lk, lv;
     lk.setup(lane, A.s.octets, A.k.token);
     lv.setup(lane, A.s.octets, A.v.token);
-    unsigned char *mine = lds + wave * (4 * TILE);
-    const unsigned lds0 = (unsigned)(unsigned long long)(__attribute__((address_space(3))) unsigned char *)mine;
+    const unsigned lds0 = (unsigned)(unsigned long long)(__attribute__((address_space(3))) unsigned char *)lds;
+    const int steps = (n + AT_STAGE - 1) / AT_STAGE;
+    // (past the last step it brings that one again, so that every step waits for the same number of loads)
+    auto fill = [&](int i) __attribute__((always_inline)) {
+        const int from = min(i, steps - 1) * AT_STAGE;
+        const unsigned to = lds0 + (unsigned)(i & 1) * (2 * TILE);
+        lk.load(k, from, n - from, to);
+        lv.load(v, from, n - from, to + TILE);
+    };
+    fill(0), fill(1);
+    sl_b8 q[STEPS];
+    sl_own_row<D>(A.q.p + at.s * A.q.token + head * A.q.head, half, A.s.octets, q);
     const int plain = sl_plain_base<D>(lane), turned = sl_turned_base<D>(lane);
     sl_f16 o[BLOCKS];
 #pragma unroll
     for (int m = 0; m < BLOCKS; ++m) o[m] = sl_zero16();
     SlRunning run;
-    const int tiles = (n + KEYS - 1) / KEYS, steps = tiles > wave ? (tiles - wave + 3) / 4 : 0;
-    // (past the last step it brings that one again, so that every step waits for the same number of loads)
-    auto fill = [&](int i) __attribute__((always_inline)) {
-        const int from = (wave + 4 * min(i, steps - 1)) * KEYS;
-        const unsigned to = lds0 + (unsigned)(i & 1) * (2 * TILE);
-        lk.load(k, from, n - from, to);
-        lv.load(v, from, n - from, to + TILE);
-    };
-    if (steps > 0) fill(0), fill(1);
 #pragma unroll 1
     for (int t = 0; t < steps; ++t) {
         wait_dma<LOADS>();
-        const unsigned char *kt = mine + (t & 1) * (2 * TILE);
-        run.tile<D>(kt, kt + TILE, plain, turned, q, min(n - (wave + 4 * t) * KEYS, (int)KEYS) - 4 * half, A.s.scale2, o);
+        const unsigned char *kt = lds + (t & 1) * (2 * TILE);
+        run.tile<D>(kt, kt + TILE, plain, turned, q, min(n - t * AT_STAGE, (int)AT_STAGE) - 4 * half, A.s.scale2, o);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // (the stage has been read)
         fill(t + 2);
     }
     wait_dma<0>();
     run.sum = sl_both_sum(run.sum);
-    __syncthreads();
-    // the waves' sums through LDS: column after column, a pad of one between them
-    float *all = reinterpret_cast<float *>(lds);
-    constexpr int PITCH = D + 1;
-    float *stats = all + 4 * 32 * PITCH;
+    if (in_group >= A.s.group) return;
+    const long long place = (long long)item.tile * A.s.heads + head;
+    float *to = A.parts + place * (A.s.octets * 8) + 4 * half;
 #pragma unroll
     for (int m = 0; m < BLOCKS; ++m)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) all[(wave * 32 + (lane & 31)) * PITCH + 32 * m + 8 * (e >> 2) + 4 * half + (e & 3)] = o[m][e];
-    if (half == 0) stats[(wave * 32 + lane) * 2] = run.top, stats[(wave * 32 + lane) * 2 + 1] = run.sum;
-    __syncthreads();
-    const int heads_here = min(A.s.group - first_head, 32), dim = A.s.octets * 8;
-    for (int i = threadIdx.x; i < heads_here * dim; i += 256) {
-        const int c = i / dim, d = i % dim;
-        float m = stats[c * 2];
-#pragma unroll
-        for (int w = 1; w < 4; ++w) m = fmaxf(m, stats[(w * 32 + c) * 2]);
-        const float to = m == -INFINITY ? 0.0f : m;
-        float value = 0.0f, total = 0.0f;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float by = __builtin_amdgcn_exp2f(stats[(w * 32 + c) * 2] - to);
-            value = fmaf(all[(w * 32 + c) * PITCH + d], by, value);
-            total = fmaf(stats[(w * 32 + c) * 2 + 1], by, total);
-        }
-        const long long place = (long long)item.tile * A.s.heads + kv * A.s.group + first_head + c;
-        A.parts[place * dim + d] = value;
-        if (d == 0) A.stats[place * 2] = m, A.stats[place * 2 + 1] = total;
-    }
+        for (int g = 0; g < 4; ++g)
+            if (m * 4 + g < A.s.octets)
+                *reinterpret_cast<sl_f4 *>(to + 32 * m + 8 * g) = sl_f4{o[m][4 * g], o[m][4 * g + 1], o[m][4 * g + 2], o[m][4 * g + 3]};
+    if (half == 0) A.stats[place * 2] = run.top, A.stats[place * 2 + 1] = run.sum;
 }
 
-// One head of one sequence to a workgroup: its parts, in their order.
+// One head of one sequence to a workgroup: its parts, in their order; their weights first, 128 at a time, each in a thread of its own.
 __global__ void __launch_bounds__(128) k_token_join(TokenArgs A)
 {
+    __shared__ float weight[128], totals[2], tops[2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int s = (int)(blockIdx.x / (unsigned)A.s.heads), head = (int)(blockIdx.x % (unsigned)A.s.heads), dim = A.s.octets * 8;
     int first, n;
     sl_rows_of(A.s.k_start, A.s.k_count, s, A.s.tokens_k, first, n);
-    const unsigned part0 = (unsigned)first / A.part + (unsigned)s, parts = ((unsigned)n + A.part - 1) / A.part;
-    if ((int)threadIdx.x >= dim) return;
-    float m = -INFINITY;
-    for (unsigned i = 0; i < parts; ++i) m = fmaxf(m, A.stats[((long long)(part0 + i) * A.s.heads + head) * 2]);
-    const float to = m == -INFINITY ? 0.0f : m;
-    float value = 0.0f, total = 0.0f;
-#pragma unroll 4
-    for (unsigned i = 0; i < parts; ++i) {
-        const long long place = (long long)(part0 + i) * A.s.heads + head;
-        const float by = __builtin_amdgcn_exp2f(A.stats[place * 2] - to);
-        value = fmaf(A.parts[place * dim + threadIdx.x], by, value);
-        total = fmaf(A.stats[place * 2 + 1], by, total);
+    const long long place0 = ((long long)((unsigned)first / A.part + (unsigned)s)) * A.s.heads + head;
+    const int parts = (int)(((unsigned)n + A.part - 1) / A.part);
+    float top = -INFINITY, total = 0.0f, value = 0.0f;
+    for (int base = 0; base < parts; base += 128) {
+        const int here = min(parts - base, 128);
+        float m = -INFINITY, sum = 0.0f;
+        if (tid < here) m = A.stats[(place0 + (long long)(base + tid) * A.s.heads) * 2], sum = A.stats[(place0 + (long long)(base + tid) * A.s.heads) * 2 + 1];
+        float most = m;
+#pragma unroll
+        for (int l = 0; l < 6; ++l) most = __builtin_elementwise_maximum(most, __int_as_float(sl_partner(__float_as_int(most), l)));
+        if (lane == 0) tops[wave] = most;
+        __syncthreads();
+        most = __builtin_elementwise_maximum(__builtin_elementwise_maximum(tops[0], tops[1]), top);
+        const float ref = most == -INFINITY ? 0.0f : most, by = __builtin_amdgcn_exp2f(m - ref), before = __builtin_amdgcn_exp2f(top - ref);
+        weight[tid] = by;
+        double t = (double)(sum * by);
+        t = sl_wave_tree(t, 6);
+        if (lane == 0) totals[wave] = (float)t;
+        __syncthreads();
+        total = total * before + (totals[0] + totals[1]), value = value * before, top = most;
+        if (tid < dim) {
+            const float *p = A.parts + (place0 + (long long)base * A.s.heads) * dim + tid;
+            const long long step = (long long)A.s.heads * dim;
+            int i = 0;
+            for (; i + 8 <= here; i += 8) {
+                float x[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = p[(i + j) * step];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) value = fmaf(x[j], weight[i + j], value);
+            }
+            for (; i < here; ++i) value = fmaf(p[i * step], weight[i], value);
+        }
+        __syncthreads();
     }
-    reinterpret_cast<unsigned short *>(A.out.p + s * A.out.token + head * A.out.head)[threadIdx.x] =
-        (unsigned short)sl_bf16_bits(total == 0.0f ? 0.0f : value / total);
+    if (tid < dim)
+        reinterpret_cast<unsigned short *>(A.out.p + s * A.out.token + head * A.out.head)[tid] = (unsigned short)sl_bf16_bits(total == 0.0f ? 0.0f : value / total);
 }
 
 int check_launch()
@@ -129,16 +134,16 @@ int check_launch()
     return SL_ERR_HIP;
 }
 
-// Parts are as short as leaves about MOST_GROUPS workgroups: the number of them counts for one sequence, their evenness for many.
+// Parts are as short as leaves about MOST_WAVES of them: for one sequence their number counts, for many their evenness.
 unsigned part_size(int64_t tokens, int64_t units)
 {
     unsigned part = LEAST_PART;
-    while (part < LONGEST_PART && tokens / part * units > MOST_GROUPS) part *= 2;
+    while (part < LONGEST_PART && tokens / part * units > MOST_WAVES) part *= 2;
     return part;
 }
 int64_t most_parts(int64_t sequences, int64_t tokens, int64_t units)
 {
-    return std::min(tokens / LEAST_PART, std::max<int64_t>(MOST_GROUPS / units, tokens / LONGEST_PART)) + sequences;
+    return std::min(tokens / LEAST_PART, std::max<int64_t>(MOST_WAVES / units, tokens / LONGEST_PART)) + sequences;
 }
 int64_t unit_count(int64_t heads, int64_t kv_heads) { return kv_heads * ((heads / kv_heads + 31) / 32); }
 
@@ -176,14 +181,9 @@ int sl_attention_token(const sl_attention_shape *shape, const sl_heads *q, const
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (keys) {
         const bool narrow = A.s.octets <= 8;
-        const unsigned lds = 4u * 4 * KEYS * 2 * (narrow ? 64 : 128);
+        const unsigned lds = 4u * AT_STAGE * 2 * (narrow ? 64 : 128);
         const auto kernel = narrow ? k_token<64> : k_token<128>;
-        const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-        if (err != hipSuccess) {
-            sl_note_hip_error(err);
-            return SL_ERR_HIP;
-        }
-        hipLaunchKernelGGL(kernel, dim3(sl_item_groups(A.s.tiles, units)), dim3(256), lds, st, A, (unsigned)(units / shape->kv_heads));
+        hipLaunchKernelGGL(kernel, dim3(sl_item_groups(A.s.tiles, units)), dim3(64), lds, st, A, (unsigned)(units / shape->kv_heads));
         if (const int rc = check_launch()) return rc;
     }
     hipLaunchKernelGGL(k_token_join, dim3((unsigned)(A.s.n * A.s.heads)), dim3(128), 0, st, A);

@@ -183,28 +183,28 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) k_norm(NormArgs
 
 // ---- 4-bit matrices: 32 rows to a workgroup ----
 
-// 16 waves with two rows each; y in bf16 goes to LDS, 2048 columns at a time, from which a thread then takes blocks of 32 along a row
+// 16 waves with two rows each, OCT times eight elements of either in a lane; y in bf16 goes to LDS, 2048 columns at a time, from which a thread then takes blocks of 32 along a row
 // (q) and of 32 rows of two columns (qt): neither needs another lane, and what a wave writes lies together.
 // (LONG: more than 2048 columns, which are read twice)
-template <bool X16, int R, bool LONG>
+template <bool X16, int R, int OCT, bool LONG>
 __global__ void __launch_bounds__(1024) k_norm_mx4(NormArgs A, int pitch)
 {
     extern __shared__ __align__(16) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = sl_uniform(tid >> 6);
     const long long row0 = blockIdx.x * 32ll;
-    float h[2][4][8], s[2];
+    float h[2][OCT][8], s[2];
     double sum[2] = {0.0, 0.0};
     for (long long base = 0; base < (LONG ? A.cols : 1); base += PANEL) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const long long row = row0 + wave * 2 + i;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < OCT; ++j) {
                 const long long col = base + (j * 64 + lane) * 8;
                 form_h<X16, R>(A, row, col, row < A.rows ? octet_left(A.cols, col) : 0, h[i][j]);
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < OCT; ++j) {
                 const long long col = base + (j * 64 + lane) * 8;
                 if constexpr (R != NONE) put_octet(A.h, R == B16, row * A.ldh + col, row < A.rows ? octet_left(A.cols, col) : 0, h[i][j]);
                 sum[i] = sum[i] + square_sum(h[i][j]);
@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(1024) k_norm_mx4(NormArgs A, int pitch)
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < OCT; ++j) {
                 const long long row = row0 + wave * 2 + i, col = base + (j * 64 + lane) * 8;
                 const int n = row < A.rows ? octet_left(A.cols, col) : 0;
                 if constexpr (LONG) {
@@ -400,8 +400,10 @@ __global__ void __launch_bounds__(1024) k_join_dw(const float *parts, int groups
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const long long col = blockIdx.x * 64ll + lane;
     double t = 0.0;
-    if (col < cols)
+    if (col < cols) {
+#pragma unroll 8
         for (int g = wave; g < groups; g += 16) t = t + (double)parts[g * cols + col];
+    }
     room[wave][lane] = t;
     __syncthreads();
     if (wave > 0 || col >= cols) return;
@@ -432,7 +434,7 @@ int launch_norm(const NormArgs &A, hipStream_t st)
         const int pitch = 2 * (int)std::min<long long>((A.cols + MX_COLS - 1) / MX_COLS * MX_COLS, PANEL) + 16;
         const unsigned groups = (unsigned)(A.qt ? (A.rows + 127) / 128 * 4 : (A.rows + 63) / 64 * 2), bytes = 32u * pitch;
         typedef void (*kernel_t)(NormArgs, int);
-        const kernel_t k = wide ? k_norm_mx4<X16, R, true> : k_norm_mx4<X16, R, false>;
+        const kernel_t k = wide ? k_norm_mx4<X16, R, 4, true> : A.cols > 512 ? k_norm_mx4<X16, R, 4, false> : k_norm_mx4<X16, R, 1, false>;
         if (bytes > 65536) {
             const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
             if (err != hipSuccess) {
