@@ -372,7 +372,8 @@ SL_DEV sl_f16 sl_four_blocks(const float *room, int stride, int lane, sl_f4 by)
 
 const int64_t AT_MOST_TOKENS = (int64_t)1 << 30, AT_MOST_HEADS = 1 << 16, AT_MOST_SEQUENCES = (int64_t)1 << 22, AT_MOST_STRIDE = (int64_t)1 << 24;
 
-// False where the shape is none.  (A grid has less than 2^32 threads: 2^24 workgroups of 256.)
+// False where the shape is none.  (A grid has less than 2^32 threads: 2^24 workgroups of 256.  The queries that a key is walked past, 32 at a time in all
+// heads of its group, are then less than 2^27.)
 inline bool sl_attention_sequences(const sl_attention_shape *p, SlSequences &s)
 {
     if (!p || p->sequences < 0 || p->sequences > AT_MOST_SEQUENCES || p->tokens_q < 0 || p->tokens_q > AT_MOST_TOKENS || p->tokens_k < 0 || p->tokens_k > AT_MOST_TOKENS)

@@ -243,3 +243,72 @@ def test_starts_outside_the_tokens_are_cut_off():
             one = torch.full((5, 2, 64), 9.0, device="cuda", dtype=torch.bfloat16)
             sl.sl_attention_token(q[:3], k, v, one[1:4], s, c, workspace=sl.alloc_attention_token_workspace(3, 200, 2, 1, 64))
             assert bool((one[[0, 4]] == 9).all())
+
+
+# ---- long lists: workgroups of 128 rows ----
+
+@pytest.mark.parametrize("dim", [40, 64, 104, 128])
+@pytest.mark.parametrize("length", [1, 63, 64, 65, 127, 128, 129, 200, 257, 385])
+def test_many_heads(length, dim):
+    """Enough heads for workgroups of 128 rows; a few of the heads are compared, all of them are finite."""
+    import torch
+    from paper_2508_15706_amd import binding as sl
+    heads = 200
+    q, k, v, dout = tensors(length, length, heads, heads, dim, seed=length)
+    s = starts([length])
+    out, lse = torch.empty(length, heads, dim, device="cuda", dtype=torch.bfloat16), torch.empty(heads, length, device="cuda")
+    dq, dk, dv = (torch.empty_like(out) for _ in range(3))
+    sl.sl_attention(q, k, v, out, s, lse=lse)
+    sl.sl_attention_backward(q, k, v, out, lse, dout, dq, dk, dv, s, workspace=sl.alloc_attention_workspace(length, heads))
+    for h in (0, 1, 24, 25, 100, 191, 192, 199):
+        r = ref.attention(q[:, h], k[:, h], v[:, h], True, dim ** -0.5, dout[:, h])
+        for name, t in (("out", out), ("dq", dq), ("dk", dk), ("dv", dv)):
+            assert worst(t[:, h], r[name], r[name + "_off"]) <= 1.0, (name, h)
+        assert bool(((lse[h].double() - r["lse"]).abs() <= r["lse_off"]).all())
+    assert all(bool(t.isfinite().all()) for t in (out, lse, dq, dk, dv))
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("causal", [True, False])
+def test_many_sequences_of_both_lengths(dim, causal):
+    """Workgroups of 128 rows with fewer queries than keys, more, none, and grouped heads."""
+    qn, kn = [3, 130, 200, 0, 17, 65, 1, 260], [200, 300, 70, 40, 0, 64, 193, 260]
+    q, k, v, dout = tensors(sum(qn), sum(kn), 48, 24, dim, seed=3)
+    check(q, k, v, dout, qn, kn, causal, None)
+
+
+@pytest.mark.parametrize("n", [63, 64, 65, 256, 257, 400])
+def test_numbers_of_sequences(n):
+    """Lists that are ordered by work and lists that are too many for it."""
+    lengths = [(7 * i) % 41 for i in range(n)]
+    q, k, v, dout = tensors(sum(lengths), sum(lengths), 1, 1, 64, seed=n)
+    check(q, k, v, dout, lengths, lengths, True, None)
+
+
+def test_offsets_beyond_32_bits():
+    """Keys, values and queries whose elements lie more than 2^31 elements into their tensors; a cache of which the last rows are used."""
+    import torch
+    from paper_2508_15706_amd import binding as sl
+    heads, dim, tokens = 40, 128, 440_000                      # 2.25e9 elements, 4.5 GB
+    k = torch.zeros(tokens, heads, dim, device="cuda", dtype=torch.bfloat16)
+    q, v, dout = torch.zeros_like(k), torch.zeros_like(k), torch.zeros_like(k)
+    lengths = [tokens - 300, 200, 100]
+    s = starts(lengths)
+    for t, seed in ((q, 1), (k, 2), (v, 3), (dout, 4)):
+        t[-300:].normal_(0, 1, generator=torch.Generator(device="cuda").manual_seed(seed))
+    few = starts([0, 200, 100], tokens - 300)                  # (the long sequence itself is left out of the attention)
+    out, lse = torch.empty(tokens, heads, dim, device="cuda", dtype=torch.bfloat16), torch.empty(heads, tokens, device="cuda")
+    sl.sl_attention(q, k, v, out, few, lse=lse)
+    dq, dk, dv = (torch.empty_like(k) for _ in range(3))
+    sl.sl_attention_backward(q, k, v, out, lse, dout, dq, dk, dv, few, workspace=sl.alloc_attention_workspace(tokens, heads))
+    one = torch.empty(3, heads, dim, device="cuda", dtype=torch.bfloat16)
+    count = torch.tensor([1, 200, 100], dtype=torch.int32, device="cuda")
+    sl.sl_attention_token(q[-3:], k, v, one, s, count, workspace=sl.alloc_attention_token_workspace(3, tokens, heads, heads, dim))
+    for i, (a, n) in enumerate(((tokens - 300, 200), (tokens - 100, 100))):
+        rows = slice(a, a + n)
+        for h in (0, 17, 39):
+            r = ref.attention(q[rows, h], k[rows, h], v[rows, h], True, dim ** -0.5, dout[rows, h])
+            for name, t in (("out", out), ("dq", dq), ("dk", dk), ("dv", dv)):
+                assert worst(t[rows, h], r[name], r[name + "_off"]) <= 1.0, (name, i, h)
+            r = ref.attention(q[tokens - 2 + i: tokens - 1 + i, h] if i == 0 else q[tokens - 1:, h], k[rows, h], v[rows, h], False, dim ** -0.5)
+            assert worst(one[i + 1: i + 2, h], r["out"], r["out_off"]) <= 1.0, ("token", i, h)

@@ -164,3 +164,22 @@ def test_rows_are_apart():
     want = torch.empty(40, 96, device="cuda")
     sl.sl_mx4_dequantize(q2, want)
     assert torch.equal(dense[rest], want[rest]) and bool(dense[4].isnan().all())
+
+
+def test_offsets_beyond_32_bits():
+    import torch
+    from paper_2508_15706_amd import binding as sl
+    rows, cols = 1_100_000, 2000                               # 2.2e9 elements
+    x = torch.zeros(rows, cols, device="cuda", dtype=torch.bfloat16)
+    x[-40:] = rand((40, cols), "bf16", 1)
+    w = rand((1, cols), "f32", 3)[0].contiguous()
+    y, s = torch.empty_like(x), torch.empty(rows, device="cuda")
+    sl.sl_rms_norm(x, w, y, rstd=s, eps=EPS)
+    _, es, ey = ref.norm(x[-40:], None, w, EPS, torch.bfloat16)
+    near(y[-40:], ey, 3 * ref.F32 * ey.abs(), ("y", torch.bfloat16))
+    assert bool((y[:100] == 0).all())
+    dx, dw = torch.empty_like(x), torch.empty(cols, device="cuda")
+    sl.sl_rms_norm_backward(x, w, s, y, dx, dw=dw, workspace=sl.alloc_rms_norm_workspace(rows, cols))
+    ex, ox, ew, ow = ref.norm_backward(x[-40:], w, s[-40:], y[-40:], None)
+    near(dx[-40:], ex, ox, ("dx", torch.bfloat16))
+    near(dw, ew, ow, ("dw", torch.float32))

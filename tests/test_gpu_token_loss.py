@@ -126,3 +126,17 @@ def test_borders_of_the_range():
     each[6] = 0.0
     want = -(weights.double() * each).sum()
     assert abs(float(loss) - float(want)) < 1e-5 * float((weights.double() * each.abs()).sum())
+
+
+def test_offsets_beyond_32_bits():
+    import torch
+    from paper_2508_15706_amd import binding as sl
+    rows, vocab = 45_000, 50_257                               # 2.26e9 elements
+    z = torch.zeros(rows, vocab, device="cuda", dtype=torch.bfloat16)
+    z[-3:], targets, weights = inputs(3, vocab, "bf16")[0], torch.full((rows,), -1, device="cuda"), torch.ones(rows, device="cuda")
+    targets[-3:] = torch.tensor([0, vocab - 1, 777], device="cuda")
+    loss, logp = torch.empty(1, device="cuda"), torch.empty(rows, device="cuda")
+    tail, last = z[-3:].clone(), targets[-3:]
+    sl.sl_token_loss(z, targets, weights, loss, logp=logp, dlogits=z, workspace=sl.alloc_token_loss_workspace(rows))
+    check(tail, last, weights[-3:], None, loss, logp[-3:], z[-3:])
+    assert bool((z[0] == 0).all()) and bool((logp[:-3] == 0).all())
