@@ -735,6 +735,20 @@ def _on_current_device(*tensors: Optional[torch.Tensor]) -> None:
             raise ValueError(f"expected tensors on the current device ({here}), got one on {t.device}")
 
 
+def _second(what: str, t: Optional[torch.Tensor], shape, dtype=None):
+    """(pointer, type, row stride) of a device matrix of a shape that is known, or of none."""
+    if t is None:
+        return None, 0, 0
+    typ = _TYPES.get(t.dtype)
+    if t.shape != shape or (dtype is not None and t.dtype is not dtype):
+        _same(what, t, shape, dtype)
+    ld, step = t.stride()
+    rows, cols = shape
+    if typ is None or not t.is_cuda or (step != 1 and cols > 1):
+        raise ValueError(f"{what}: expected a float32 or bfloat16 device matrix with contiguous rows")
+    return t.data_ptr(), typ, (ld if rows > 1 else max(cols, ld))
+
+
 @functools.lru_cache(maxsize=4096)
 def sl_rms_norm_workspace_bytes(rows: int, cols: int) -> int:
     return int(lib().sl_rms_norm_workspace_bytes(int(rows), int(cols)))
@@ -749,19 +763,12 @@ def sl_rms_norm(x: torch.Tensor, weight: torch.Tensor, y: Optional[torch.Tensor]
                 qt: Optional[torch.Tensor] = None, eps: float = 1e-5, stream=None) -> None:
     """h = x + residual; y = h / rms(h) * weight, dense and (q, qt) as 4-bit matrices of its rows and columns; rstd = 1 / rms."""
     xp, xt, rows, cols, ldx = _matrix(x)
-    rp, rt, ldr, hp, ht, ldh = None, 0, 0, None, 0, 0
     if (residual is None) != (h is None):
         raise ValueError("residual and h go together")
     _same("weight", weight, (cols,))
-    _same("y", y, x.shape)
-    if h is not None:
-        _same("residual", residual, x.shape)
-        _same("h", h, x.shape, residual.dtype)
-        rp, rt, _, _, ldr = _matrix(residual)
-        hp, ht, _, _, ldh = _matrix(h)
-    yp, yt, ldy = None, 0, 0
-    if y is not None:
-        yp, yt, _, _, ldy = _matrix(y)
+    rp, _, ldr = _second("residual", residual, x.shape)
+    hp, ht, ldh = _second("h", h, x.shape, None if residual is None else residual.dtype)
+    yp, yt, ldy = _second("y", y, x.shape)
     _on_current_device(x, weight, y, residual, h, rstd, q, qt)
     st = lib().sl_rms_norm(xp, xt, ldx, rp, ldr, hp, ht, ldh, _dev_ptr(weight), _type_of(weight), rows, cols, float(eps), yp, yt, ldy,
                            _room("rstd", rstd, rows, torch.float32), _mx4_ptr(q, rows, cols), _mx4_ptr(qt, cols, rows), _stream_ptr(stream))
@@ -775,15 +782,10 @@ def sl_rms_norm_backward(h: torch.Tensor, weight: torch.Tensor, rstd: torch.Tens
     """dx: gradient of x (and of the residual) from dy and from dh, which reaches h past the norm; dw: fp32, or None."""
     hp, ht, rows, cols, ldh = _matrix(h)
     _same("weight", weight, (cols,))
-    _same("dy", dy, h.shape)
-    _same("dx", dx, h.shape)
-    _same("dh", dh, h.shape, dx.dtype)
     _same("dw", dw, (cols,), torch.float32)
-    gp, gt, _, _, ldg = _matrix(dy)
-    op, ot, _, _, ldo = _matrix(dx)
-    ip, ldi = None, 0
-    if dh is not None:
-        ip, _, _, _, ldi = _matrix(dh)
+    gp, gt, ldg = _second("dy", dy, h.shape)
+    op, ot, ldo = _second("dx", dx, h.shape)
+    ip, _, ldi = _second("dh", dh, h.shape, dx.dtype)
     _on_current_device(h, weight, rstd, dy, dx, dh, dw, workspace)
     st = lib().sl_rms_norm_backward(hp, ht, ldh, _dev_ptr(weight), _type_of(weight), _room("rstd", rstd, rows, torch.float32), gp, gt, ldg,
                                     ip, ldi, op, ot, ldo, _dev_ptr(dw), int(accumulate), rows, cols,
@@ -794,7 +796,8 @@ def sl_rms_norm_backward(h: torch.Tensor, weight: torch.Tensor, rstd: torch.Tens
 
 
 def _heads(what: str, t: torch.Tensor, shape) -> SlHeads:
-    _same(what, t, shape, torch.bfloat16)
+    if t.shape != shape or t.dtype is not torch.bfloat16:
+        _same(what, t, shape, torch.bfloat16)
     token, head, step = t.stride()
     if not t.is_cuda or step != 1:
         raise ValueError(f"{what}: expected a device tensor whose heads are contiguous")
@@ -905,10 +908,7 @@ def sl_token_loss(logits: torch.Tensor, targets: torch.Tensor, weights: Optional
     _same("targets", targets, (rows,), torch.int64)
     _same("weights", weights, (rows,), torch.float32)
     _same("logp", logp, (rows,), torch.float32)
-    _same("dlogits", dlogits, logits.shape, logits.dtype)
-    dp, ldd = None, 0
-    if dlogits is not None:
-        dp, _, _, _, ldd = _matrix(dlogits)
+    dp, _, ldd = _second("dlogits", dlogits, logits.shape, logits.dtype)
     pol = None
     if policy is not None:
         for what in ("old_logp", "advantage", "ref_logp"):
