@@ -18,7 +18,8 @@
  * Top-k"): sl_compress_coded / sl_decompress_avg_apply_coded.
  *
  * What a worker computes between two outer steps (Algorithm 1, inner loop) is here too:
- * linear layers on microscaled 4-bit operands with both gradients (sl_mx4_*), the norm that
+ * linear layers on microscaled 4-bit operands with both gradients (sl_mx4_*), the layers between
+ * them (sl_rms_norm, sl_attention, sl_token_loss and their backward passes), the norm that
  * the gradients are clipped by (sl_grad_norm) and AdamW (sl_adamw_*), see "The inner step".
  *
  * Conventions for every function

@@ -11,6 +11,7 @@
 #include "sl_dma.h"
 #include "sl_mx4.h"
 
+#include <climits>
 #include <cmath>
 
 #include "sl_internal.h"
@@ -67,31 +68,49 @@ SL_DEV bool sl_find_tile(const int *start, int n, int tokens, unsigned rows, uns
     out.s = lo, out.first = a, out.count = b - a, out.row0 = (int)row0;
     return row0 >= 0 && row0 < b - a;
 }
+// Rows of a sequence on one side; `count`: how many of them are used, or null.
+SL_DEV void sl_rows_of(const int *start, const int *count, int s, int tokens, int &first, int &n)
+{
+    const int a = min(max(start[s], 0), tokens), b = min(max(start[s + 1], a), tokens);
+    first = a;
+    n = count ? min(max(count[s], 0), b - a) : b - a;
+}
+
+// The sum over the wave's lanes, in all of them (and known to be the same).
+SL_DEV int sl_wave_sum(int v)
+{
+#pragma unroll
+    for (int l = 0; l < 4; ++l) v += sl_partner(v, l);
+    return (__builtin_amdgcn_readlane(v, 0) + __builtin_amdgcn_readlane(v, 16)) + (__builtin_amdgcn_readlane(v, 32) + __builtin_amdgcn_readlane(v, 48));
+}
+
 // The same by work: where queries see only keys before them, a sequence's tile `level` from its light end is `level` tiles' work more than the
 // lightest, and a workgroup that begins with a heavy tile late keeps the others waiting.  Item t is the t-th of all sequences' tiles in
 // descending order of their levels.  Each lane holds PER sequences' numbers of tiles; the sum of max(tiles - level, 0) over them is
 // the number of tiles of that level or more.  Lists of more sequences than that have enough tiles for the order not to count.
-// (eight sequences of 2048 tokens, forward: 209 us in the sequences' order)
+// (eight sequences of 2048 tokens, forward: 209 us in the sequences' order, so 177)
+// What belongs to a sequence is requested by its lane at the start, all of it at once, and then read from the lane.
 template <int PER>
-SL_DEV bool sl_find_level(const int *start, int n, int tokens, unsigned rows, unsigned t, bool light_first, SlSpan &out)
+SL_DEV bool sl_find_level(const int *start, int tokens, const int *other_start, const int *other_count, int other_tokens, int n, unsigned rows, unsigned t,
+                          bool light_first, SlSpan &out, int &other_first, int &other_n)
 {
     const int lane = threadIdx.x & 63;
-    int tiles[PER], most = 0;
+    int first[PER], count[PER], of[PER], on[PER], tiles[PER], most = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        const int s = i * 64 + lane;
-        const int a = s < n ? min(max(start[s], 0), tokens) : 0, b = s < n ? min(max(start[s + 1], a), tokens) : 0;
-        tiles[i] = (int)(((unsigned)(b - a) + rows - 1) / rows);
+        const int s = min(i * 64 + lane, n - 1);
+        const int a = start[s], b = start[s + 1], c = other_start[s], d = other_start[s + 1], e = other_count ? other_count[s] : INT_MAX;
+        first[i] = min(max(a, 0), tokens), count[i] = min(max(b, first[i]), tokens) - first[i];
+        of[i] = min(max(c, 0), other_tokens), on[i] = min(max(e, 0), min(max(d, of[i]), other_tokens) - of[i]);
+        tiles[i] = i * 64 + lane < n ? (int)(((unsigned)count[i] + rows - 1) / rows) : 0;
         most = max(most, tiles[i]);
     }
-    most = sl_uniform(sl_wave_max(most));
+    most = sl_wave_max(most);
     auto reach = [&](int level) __attribute__((always_inline)) {        // tiles of that level or more
         int c = 0;
 #pragma unroll
         for (int i = 0; i < PER; ++i) c += max(tiles[i] - level, 0);
-#pragma unroll
-        for (int l = 0; l < 6; ++l) c += sl_partner(c, l);
-        return (unsigned)sl_uniform(c);
+        return (unsigned)sl_wave_sum(c);
     };
     int lo = 0, hi = most;                       // reach(lo) > t >= reach(hi)
     if (reach(0) <= t) return false;
@@ -106,29 +125,25 @@ SL_DEV bool sl_find_level(const int *start, int n, int tokens, unsigned rows, un
         const unsigned long long has = sl_ballot(tiles[i] > lo);
         const unsigned c = (unsigned)sl_popc(has);
         if (left < c) {
-            const int s = sl_uniform(i * 64 + __builtin_ctzll(sl_ballot(tiles[i] > lo && (unsigned)sl_mbcnt(has) == left)));
-            const int a = min(max(start[s], 0), tokens), b = min(max(start[s + 1], a), tokens);
-            out.s = s, out.first = a, out.count = b - a;
-            out.row0 = (light_first ? lo : (int)(((unsigned)(b - a) + rows - 1) / rows) - 1 - lo) * (int)rows;
+            const int l = sl_uniform(__builtin_ctzll(sl_ballot(tiles[i] > lo && (unsigned)sl_mbcnt(has) == left)));
+            out.s = i * 64 + l, out.first = __builtin_amdgcn_readlane(first[i], l), out.count = __builtin_amdgcn_readlane(count[i], l);
+            out.row0 = (light_first ? lo : __builtin_amdgcn_readlane(tiles[i], l) - 1 - lo) * (int)rows;
+            other_first = __builtin_amdgcn_readlane(of[i], l), other_n = __builtin_amdgcn_readlane(on[i], l);
             return true;
         }
         left -= c;
     }
     return false;
 }
-SL_DEV bool sl_find(const int *start, int n, int tokens, unsigned rows, unsigned tiles, unsigned t, bool light_first, SlSpan &out)
+// Item t of the list's tiles of `rows` rows, and the rows of its sequence on the other side, of which `other_count` (or null) says how many are used.
+SL_DEV bool sl_find(const int *start, int tokens, const int *other_start, const int *other_count, int other_tokens, const SlSequences &s, unsigned rows, unsigned t,
+                    bool light_first, SlSpan &out, int &other_first, int &other_n)
 {
-    if (n <= 64) return sl_find_level<1>(start, n, tokens, rows, t, light_first, out);
-    if (n <= 256) return sl_find_level<4>(start, n, tokens, rows, t, light_first, out);
-    return sl_find_tile(start, n, tokens, rows, light_first ? tiles - 1 - t : t, out);
-}
-
-// Rows of a sequence on one side; `count`: how many of them are used, or null.
-SL_DEV void sl_rows_of(const int *start, const int *count, int s, int tokens, int &first, int &n)
-{
-    const int a = min(max(start[s], 0), tokens), b = min(max(start[s + 1], a), tokens);
-    first = a;
-    n = count ? min(max(count[s], 0), b - a) : b - a;
+    if (s.n <= 64) return sl_find_level<1>(start, tokens, other_start, other_count, other_tokens, s.n, rows, t, light_first, out, other_first, other_n);
+    if (s.n <= 256) return sl_find_level<4>(start, tokens, other_start, other_count, other_tokens, s.n, rows, t, light_first, out, other_first, other_n);
+    if (!sl_find_tile(start, s.n, tokens, rows, light_first ? s.tiles - 1 - t : t, out)) return false;
+    sl_rows_of(other_start, other_count, out.s, other_tokens, other_first, other_n);
+    return true;
 }
 
 // ---- tiles in LDS ----
@@ -236,7 +251,7 @@ SL_DEV sl_f16 sl_zero16()
 }
 
 // The order of N products, each with one read of LDS: AHEAD reads first, then one for each product.  (Left to itself the compiler waits for
-// every pair of reads in front of its products: forward pass over 8192 tokens 390 us, so 315.)
+// every pair of reads in front of its products: forward pass over 8192 tokens, 20 heads of 128, 389 us, so 357.)
 template <int N, int AHEAD>
 SL_DEV void sl_reads_ahead()
 {

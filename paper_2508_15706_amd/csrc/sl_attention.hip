@@ -28,9 +28,12 @@ struct BackArgs {
 
 // ---- forward ----
 
-// 128 queries of one head, 32 to a wave, over 64 keys at a time, two stages of LDS.  The running maximum moves only where a row's new one is
-// more than 2^8 above it: the sum and the output then stay below 2^8 times their values, and the output's registers are scaled a
-// few times in all.
+// 128 queries of one head, 32 to a wave, over 64 keys at a time, two stages of LDS; the softmax in one pass, as in SlRunning (whose 32 keys
+// would leave the matrix unit one chain of products; here are two).  Two workgroups to a compute unit: 32 products of 32 cycles a wave and
+// 64 keys stand against about 1000 cycles of exponentials, sums and maxima, and the one's run beside the other's.
+// 8192 tokens, 20 heads of 128 on 5: 353 us, 0.97 PFLOP/s at 2.0 GHz; 8 x 2048 tokens, 16 heads: 175 us, 0.79 - the same loop on constant operands
+// in LDS, without masks, starts and ends: 1630 ns for 64 keys of two waves at 2.4 GHz, here 2170.  Tried and not kept: the next tile's scores beside this
+// one's exponentials in the same wave (111 registers spilled, 704 us), priorities of waves around products or exponentials (the same time).
 template <int D>
 __global__ void __launch_bounds__(256, 2) k_attend(AttendArgs A)
 {
@@ -39,9 +42,8 @@ __global__ void __launch_bounds__(256, 2) k_attend(AttendArgs A)
     const SlItem item = sl_item(blockIdx.x, (unsigned)A.s.heads);
     if (item.tile >= A.s.tiles) return;
     SlSpan at;
-    if (!sl_find(A.s.q_start, A.s.n, A.s.tokens_q, AT_ROWS, A.s.tiles, item.tile, true, at)) return;
     int k0, kn;
-    sl_rows_of(A.s.k_start, A.s.k_count, at.s, A.s.tokens_k, k0, kn);
+    if (!sl_find(A.s.q_start, A.s.tokens_q, A.s.k_start, A.s.k_count, A.s.tokens_k, A.s, AT_ROWS, item.tile, true, at, k0, kn)) return;
     const int lane = threadIdx.x & 63, wave = sl_uniform((int)(threadIdx.x >> 6)), half = lane >> 5;
     const int head = (int)item.head, kv = head / A.s.group, shift = kn - at.count;
     const int row = at.row0 + wave * 32 + (lane & 31), mine = min(row, at.count - 1);
@@ -142,9 +144,8 @@ __global__ void __launch_bounds__(256, 1) k_attend_few(AttendArgs A)
     const SlItem item = sl_item(blockIdx.x, (unsigned)A.s.heads);
     if (item.tile >= A.s.tiles) return;
     SlSpan at;
-    if (!sl_find(A.s.q_start, A.s.n, A.s.tokens_q, 32, A.s.tiles, item.tile, true, at)) return;
     int k0, kn;
-    sl_rows_of(A.s.k_start, A.s.k_count, at.s, A.s.tokens_k, k0, kn);
+    if (!sl_find(A.s.q_start, A.s.tokens_q, A.s.k_start, A.s.k_count, A.s.tokens_k, A.s, 32, item.tile, true, at, k0, kn)) return;
     const int lane = threadIdx.x & 63, wave = sl_uniform((int)(threadIdx.x >> 6)), half = lane >> 5;
     const int head = (int)item.head, kv = head / A.s.group, shift = kn - at.count;
     const int row = at.row0 + (lane & 31), mine = min(row, at.count - 1);
@@ -211,6 +212,8 @@ __global__ void __launch_bounds__(256, 1) k_attend_few(AttendArgs A)
 // ---- backward ----
 
 // dq: queries to lanes as in the forward pass; S and dP of 32 keys at a time.  It also leaves what the pass over keys needs of a query.
+// Three products where the pass over keys has four; 8 x 2048 tokens, 16 heads of 128: 232 us, 0.89 PFLOP/s.  (dq from that pass would need
+// sums over workgroups, in memory or in an order that changes.)
 // sum dout out is that of P dP, too: for queries that see few keys, whose dP - sum dout out is small beside its terms, it is taken from there,
 // in a pass over the keys in front.  From out, which is rounded, it moves the dS of all of a query's keys the same way, by its own
 // rounding's share of |dout| |out|, which does not average out over few keys (1024 tokens, N(0, 1.5) queries: dq's error 0.28 % of its norm
@@ -226,9 +229,8 @@ __global__ void __launch_bounds__(256, 2) k_back_q(BackArgs A)
     if (blockIdx.x == 0 && threadIdx.x < 2) A.stats[A.none + threadIdx.x] = threadIdx.x == 0 ? INFINITY : 0.0f;
     if (item.tile >= A.s.tiles) return;
     SlSpan at;
-    if (!sl_find(A.s.q_start, A.s.n, A.s.tokens_q, AT_ROWS, A.s.tiles, item.tile, true, at)) return;
     int k0, kn;
-    sl_rows_of(A.s.k_start, A.s.k_count, at.s, A.s.tokens_k, k0, kn);
+    if (!sl_find(A.s.q_start, A.s.tokens_q, A.s.k_start, A.s.k_count, A.s.tokens_k, A.s, AT_ROWS, item.tile, true, at, k0, kn)) return;
     const int lane = threadIdx.x & 63, wave = sl_uniform((int)(threadIdx.x >> 6)), half = lane >> 5;
     const int head = (int)item.head, kv = head / A.s.group, shift = kn - at.count;
     const int row = at.row0 + wave * 32 + (lane & 31), mine = min(row, at.count - 1);
@@ -338,9 +340,8 @@ __global__ void __launch_bounds__(256, 1) k_back_q_few(BackArgs A)
     if (blockIdx.x == 0 && threadIdx.x < 2) A.stats[A.none + threadIdx.x] = threadIdx.x == 0 ? INFINITY : 0.0f;
     if (item.tile >= A.s.tiles) return;
     SlSpan at;
-    if (!sl_find(A.s.q_start, A.s.n, A.s.tokens_q, 32, A.s.tiles, item.tile, true, at)) return;
     int k0, kn;
-    sl_rows_of(A.s.k_start, A.s.k_count, at.s, A.s.tokens_k, k0, kn);
+    if (!sl_find(A.s.q_start, A.s.tokens_q, A.s.k_start, A.s.k_count, A.s.tokens_k, A.s, 32, item.tile, true, at, k0, kn)) return;
     const int lane = threadIdx.x & 63, wave = sl_uniform((int)(threadIdx.x >> 6)), half = lane >> 5;
     const int head = (int)item.head, kv = head / A.s.group, shift = kn - at.count;
     const int row = at.row0 + (lane & 31), mine = min(row, at.count - 1);
@@ -465,7 +466,8 @@ SL_DEV void back_scores(sl_f16 &s, sl_f16 &dp, const float *stats, int from, flo
 
 // dk and dv: 128 keys of one key head, 32 to a wave, over all queries of the heads that share it, 32 at a time; the sums over the heads are
 // made in registers, in their order.  A wave holds its keys in registers and its values in LDS, so that two workgroups fit a compute unit
-// and one's exponentials run beside the other's products.
+// and one's exponentials run beside the other's products: 8 x 2048 tokens, 16 heads of 128, 320 us, 0.86 PFLOP/s (keys and values in registers, one
+// workgroup to a compute unit, 412).
 template <int D>
 __global__ void __launch_bounds__(256, 2) k_back_kv(BackArgs A)
 {
@@ -475,10 +477,9 @@ __global__ void __launch_bounds__(256, 2) k_back_kv(BackArgs A)
     const SlItem item = sl_item(blockIdx.x, (unsigned)kv_heads);
     if (item.tile >= A.s.tiles) return;
     SlSpan at;
-    if (!sl_find(A.s.k_start, A.s.n, A.s.tokens_k, AT_ROWS, A.s.tiles, item.tile, false, at)) return;
-    int q0, qn, k0, kn;
-    sl_rows_of(A.s.q_start, nullptr, at.s, A.s.tokens_q, q0, qn);
-    sl_rows_of(A.s.k_start, A.s.k_count, at.s, A.s.tokens_k, k0, kn);
+    int q0, qn;
+    if (!sl_find(A.s.k_start, A.s.tokens_k, A.s.q_start, nullptr, A.s.tokens_q, A.s, AT_ROWS, item.tile, false, at, q0, qn)) return;
+    const int k0 = at.first, kn = A.s.k_count ? min(max(A.s.k_count[at.s], 0), at.count) : at.count;
     if (at.row0 >= kn) return;
     const int lane = threadIdx.x & 63, wave = sl_uniform((int)(threadIdx.x >> 6)), half = lane >> 5;
     const int kv = (int)item.head, shift = kn - qn;
@@ -586,10 +587,9 @@ __global__ void __launch_bounds__(256, 1) k_back_kv_few(BackArgs A)
     const SlItem item = sl_item(blockIdx.x, (unsigned)kv_heads);
     if (item.tile >= A.s.tiles) return;
     SlSpan at;
-    if (!sl_find(A.s.k_start, A.s.n, A.s.tokens_k, 32, A.s.tiles, item.tile, false, at)) return;
-    int q0, qn, k0, kn;
-    sl_rows_of(A.s.q_start, nullptr, at.s, A.s.tokens_q, q0, qn);
-    sl_rows_of(A.s.k_start, A.s.k_count, at.s, A.s.tokens_k, k0, kn);
+    int q0, qn;
+    if (!sl_find(A.s.k_start, A.s.tokens_k, A.s.q_start, nullptr, A.s.tokens_q, A.s, 32, item.tile, false, at, q0, qn)) return;
+    const int k0 = at.first, kn = A.s.k_count ? min(max(A.s.k_count[at.s], 0), at.count) : at.count;
     if (at.row0 >= kn) return;
     const int lane = threadIdx.x & 63, wave = sl_uniform((int)(threadIdx.x >> 6)), half = lane >> 5;
     const int kv = (int)item.head, shift = kn - qn;
