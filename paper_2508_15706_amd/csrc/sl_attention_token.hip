@@ -18,8 +18,8 @@ struct TokenArgs {
 
 // A part of a sequence's keys for up to 32 heads that share a key head: the heads are the columns of the score tile.  One wave does it, 32
 // keys at a time, in two stages of LDS, and waits for nobody: five of them fit a compute unit, so that one's start and end lie beside
-// the others' loads.  Bound by the cache's bytes; the matrix unit idles.  (64 sequences, up to 16,384 keys, 5 heads of 128 - 596 MB: four waves to a
-// part of 2048 keys 122 us, of 512 183.)
+// the others' loads.  Bound by the cache's bytes; the matrix unit idles.  64 sequences, up to 16,384 keys, 5 heads of 128 - 596 MB: 114 us, 5.2
+// TB/s (parts of 256 and 1024 keys 123 and 124; four waves to a part of 2048 122, of 512 183).
 template <int D>
 __global__ void __launch_bounds__(64, 2) k_token(TokenArgs A, unsigned blocks)
 {
