@@ -554,8 +554,8 @@ typedef struct {                               /* element (t, h, d) at data + t*
 int sl_attention(const sl_attention_shape *shape, const sl_heads *q, const sl_heads *k, const sl_heads *v, const sl_heads *out, float *lse,
                  void *stream);
 /* Gradients from that of out: dq like q, dk and dv like k and v, each summed over the heads that share it, in a fixed order.
- * out, lse   in, as sl_attention left them;  workspace: device, sl_attention_workspace_bytes, 16-byte aligned; that of the largest call
- *            serves smaller ones */
+ * out, lse   in, as sl_attention left them;  workspace: device, sl_attention_workspace_bytes (some 200 MB at most beyond 8 bytes a query and head:
+ *            room for parts of a group's sums), 16-byte aligned; that of the largest call serves smaller ones */
 size_t sl_attention_workspace_bytes(int64_t tokens_q, int64_t heads);
 int sl_attention_backward(const sl_attention_shape *shape, const sl_heads *q, const sl_heads *k, const sl_heads *v, const sl_heads *out,
                           const float *lse, const sl_heads *dout, const sl_heads *dq, const sl_heads *dk, const sl_heads *dv, void *workspace,

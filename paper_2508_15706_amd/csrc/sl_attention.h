@@ -363,6 +363,14 @@ SL_DEV void sl_put_row(unsigned char *row, bool there, int half, int octets, con
     for (int m = 0; m < D / 32; ++m) sl_put_block(row, there, half, octets, v[m], m, by);
 }
 
+// The same in fp32, as it is.
+SL_DEV void sl_put_floats(float *row, bool there, int half, int octets, const sl_f16 &v, int m)
+{
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+        if (there && m * 4 + g < octets) *reinterpret_cast<sl_f4 *>(row + 32 * m + 8 * g + 4 * half) = sl_f4{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
+}
+
 // A wave's block of a result to LDS and the sum of four waves' from there, in their order; 16 floats a lane, 4 KB a block.
 SL_DEV void sl_leave_block(float *room, int lane, const sl_f16 &v)
 {

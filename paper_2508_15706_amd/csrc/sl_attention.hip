@@ -24,6 +24,9 @@ struct BackArgs {
     float *stats;                // per query: lse in base 2, sum dout out; heads x tokens each.  Behind them what stands for no query: infinity, whose
                                  // probabilities are 0, and 0
     long long none;              // where
+    // keys' and values' gradients of `slices` parts of a group's heads, fp32: [slice][dk, dv][token][key head][dim]; one slice: none
+    float *parts;
+    int slices;
 };
 
 // ---- forward ----
@@ -449,6 +452,18 @@ __global__ void __launch_bounds__(256, 1) k_back_q_few(BackArgs A)
     }
 }
 
+// Which heads of its group workgroup `item` of the passes over keys walks past, and where it leaves what it finds.
+struct Slice { int kv, slice, first, heads; };
+SL_DEV Slice slice_of(const BackArgs &A, unsigned item)
+{
+    const int kv = (int)item / A.slices, slice = (int)item % A.slices, first = slice * A.s.group / A.slices;
+    return Slice{kv, slice, kv * A.s.group + first, (slice + 1) * A.s.group / A.slices - first};
+}
+SL_DEV float *part_row(const BackArgs &A, const Slice &w, int which, long long token)
+{
+    return A.parts + ((((long long)w.slice * 2 + which) * A.s.tokens_k + token) * (A.s.heads / A.s.group) + w.kv) * (A.s.octets * 8);
+}
+
 // Scores and dP of 32 queries (rows 8 j + e of a lane) into P and dS; queries before row `from` do not see the lane's key.
 SL_DEV void back_scores(sl_f16 &s, sl_f16 &dp, const float *stats, int from, float scale2)
 {
@@ -473,8 +488,7 @@ __global__ void __launch_bounds__(256, 2) k_back_kv(BackArgs A)
 {
     extern __shared__ __align__(16) unsigned char lds[];
     constexpr int VALUES = AT_ROWS * 2 * D, TILE = AT_STAGE * 2 * D, STAGE = 2 * TILE + 256, STEPS = D / 16, BLOCKS = D / 32;
-    const int kv_heads = A.s.heads / A.s.group;
-    const SlItem item = sl_item(blockIdx.x, (unsigned)kv_heads);
+    const SlItem item = sl_item(blockIdx.x, (unsigned)(A.s.heads / A.s.group * A.slices));
     if (item.tile >= A.s.tiles) return;
     SlSpan at;
     int q0, qn;
@@ -482,7 +496,8 @@ __global__ void __launch_bounds__(256, 2) k_back_kv(BackArgs A)
     const int k0 = at.first, kn = A.s.k_count ? min(max(A.s.k_count[at.s], 0), at.count) : at.count;
     if (at.row0 >= kn) return;
     const int lane = threadIdx.x & 63, wave = sl_uniform((int)(threadIdx.x >> 6)), half = lane >> 5;
-    const int kv = (int)item.head, shift = kn - qn;
+    const Slice work = slice_of(A, item.head);
+    const int kv = work.kv, shift = kn - qn;
     const int key = at.row0 + wave * 32 + (lane & 31), mine = min(key, kn - 1);
     const long long token = k0 + mine;
     const unsigned lds0 = (unsigned)(unsigned long long)(__attribute__((address_space(3))) unsigned char *)lds;
@@ -503,9 +518,9 @@ __global__ void __launch_bounds__(256, 2) k_back_kv(BackArgs A)
     // the first query that sees a key of the workgroup, of the wave, this lane's key
     const int first = A.s.causal ? max(at.row0 - shift, 0) / AT_STAGE : 0, tiles = (qn + AT_STAGE - 1) / AT_STAGE;
     const int wave_first = A.s.causal ? at.row0 + wave * 32 - shift : 0, key_first = A.s.causal ? key - shift : 0;
-    const int per_head = max(tiles - first, 0), stages = per_head * A.s.group;
+    const int per_head = max(tiles - first, 0), stages = per_head * work.heads;
     auto load = [&](int i) __attribute__((always_inline)) {
-        const int head = kv * A.s.group + i / per_head, tile = (first + i % per_head) * AT_STAGE;
+        const int head = work.first + i / per_head, tile = (first + i % per_head) * AT_STAGE;
         const unsigned to = lds0 + VALUES + (unsigned)(i & 1) * STAGE;
         lq.load(A.q.p + (long long)q0 * A.q.token + head * A.q.head, tile, qn, to, wave);
         lg.load(A.dout.p + (long long)q0 * A.dout.token + head * A.dout.head, tile, qn, to + TILE, wave);
@@ -572,6 +587,15 @@ __global__ void __launch_bounds__(256, 2) k_back_kv(BackArgs A)
         }
     }
     wait_dma<0>();               // (the values, where there was no stage)
+    if (A.slices > 1) {
+        float *to_k = part_row(A, work, 0, token), *to_v = part_row(A, work, 1, token);
+#pragma unroll
+        for (int m = 0; m < BLOCKS; ++m) {
+            sl_put_floats(to_k, key < kn, half, A.s.octets, dk[m], m);
+            sl_put_floats(to_v, key < kn, half, A.s.octets, dv[m], m);
+        }
+        return;
+    }
     sl_put_row<D>(A.dk.p + token * A.dk.token + kv * A.dk.head, key < kn, half, A.s.octets, dk, A.s.scale);
     sl_put_row<D>(A.dv.p + token * A.dv.token + kv * A.dv.head, key < kn, half, A.s.octets, dv, 1.0f);
 }
@@ -583,8 +607,7 @@ __global__ void __launch_bounds__(256, 1) k_back_kv_few(BackArgs A)
 {
     extern __shared__ __align__(16) unsigned char lds[];
     constexpr int TILE = AT_STAGE * 2 * D, STAGE = 2 * TILE + 256, STEPS = D / 16, BLOCKS = D / 32, LOADS = 2 * SlWaveLoad<D>::LOADS + 1;
-    const int kv_heads = A.s.heads / A.s.group;
-    const SlItem item = sl_item(blockIdx.x, (unsigned)kv_heads);
+    const SlItem item = sl_item(blockIdx.x, (unsigned)(A.s.heads / A.s.group * A.slices));
     if (item.tile >= A.s.tiles) return;
     SlSpan at;
     int q0, qn;
@@ -592,7 +615,8 @@ __global__ void __launch_bounds__(256, 1) k_back_kv_few(BackArgs A)
     const int k0 = at.first, kn = A.s.k_count ? min(max(A.s.k_count[at.s], 0), at.count) : at.count;
     if (at.row0 >= kn) return;
     const int lane = threadIdx.x & 63, wave = sl_uniform((int)(threadIdx.x >> 6)), half = lane >> 5;
-    const int kv = (int)item.head, shift = kn - qn;
+    const Slice work = slice_of(A, item.head);
+    const int kv = work.kv, shift = kn - qn;
     const int key = at.row0 + (lane & 31), mine = min(key, kn - 1);
     const long long token = k0 + mine;
     unsigned char *own = lds + wave * (2 * STAGE);
@@ -602,9 +626,9 @@ __global__ void __launch_bounds__(256, 1) k_back_kv_few(BackArgs A)
     lg.setup(lane, A.s.octets, A.dout.token);
     const int first = A.s.causal ? max(at.row0 - shift, 0) / AT_STAGE : 0, tiles = (qn + AT_STAGE - 1) / AT_STAGE;
     const int key_first = A.s.causal ? key - shift : 0;
-    const int per_head = max(tiles - first, 0), stages = per_head * A.s.group, steps = stages > wave ? (stages - wave + 3) / 4 : 0;
+    const int per_head = max(tiles - first, 0), stages = per_head * work.heads, steps = stages > wave ? (stages - wave + 3) / 4 : 0;
     auto fill = [&](int n) __attribute__((always_inline)) {
-        const int i = wave + 4 * min(n, steps - 1), head = kv * A.s.group + i / per_head, tile = (first + i % per_head) * AT_STAGE;
+        const int i = wave + 4 * min(n, steps - 1), head = work.first + i / per_head, tile = (first + i % per_head) * AT_STAGE;
         const unsigned to = lds0 + (unsigned)(n & 1) * STAGE;
         lq.load(A.q.p + (long long)q0 * A.q.token + head * A.q.head, tile, qn - tile, to);
         lg.load(A.dout.p + (long long)q0 * A.dout.token + head * A.dout.head, tile, qn - tile, to + TILE);
@@ -659,8 +683,41 @@ __global__ void __launch_bounds__(256, 1) k_back_kv_few(BackArgs A)
     __syncthreads();
     for (int i = wave; i < 2 * BLOCKS; i += 4) {
         const sl_f16 x = sl_four_blocks(room + i * 1024, 2 * BLOCKS * 1024, lane, sl_f4{1.0f, 1.0f, 1.0f, 1.0f});
-        if (i < BLOCKS) sl_put_block(A.dk.p + token * A.dk.token + kv * A.dk.head, key < kn, half, A.s.octets, x, i, A.s.scale);
+        if (A.slices > 1) sl_put_floats(part_row(A, work, i < BLOCKS ? 0 : 1, token), key < kn, half, A.s.octets, x, i < BLOCKS ? i : i - BLOCKS);
+        else if (i < BLOCKS) sl_put_block(A.dk.p + token * A.dk.token + kv * A.dk.head, key < kn, half, A.s.octets, x, i, A.s.scale);
         else sl_put_block(A.dv.p + token * A.dv.token + kv * A.dv.head, key < kn, half, A.s.octets, x, i - BLOCKS, 1.0f);
+    }
+}
+
+// dk and dv from the slices' sums, in their order: 128 keys of one key head to a workgroup, eight elements to a thread.
+__global__ void __launch_bounds__(256) k_join_kv(BackArgs A)
+{
+    const int kv_heads = A.s.heads / A.s.group;
+    const SlItem item = sl_item(blockIdx.x, (unsigned)kv_heads);
+    if (item.tile >= A.s.tiles) return;
+    SlSpan at;
+    if (!sl_find_tile(A.s.k_start, A.s.n, A.s.tokens_k, AT_ROWS, item.tile, at)) return;
+    const int kn = A.s.k_count ? min(max(A.s.k_count[at.s], 0), at.count) : at.count, rows = min(AT_ROWS, kn - at.row0), kv = (int)item.head;
+    for (int i = threadIdx.x; i < rows * A.s.octets; i += 256) {
+        const long long token = at.first + at.row0 + i / A.s.octets;
+        const int octet = i % A.s.octets;
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+#pragma unroll 4
+            for (int slice = 0; slice < A.slices; ++slice) {
+                const float *p = part_row(A, Slice{kv, slice, 0, 0}, which, token) + octet * 8;
+                const sl_f4 a = *reinterpret_cast<const sl_f4 *>(p), b = *reinterpret_cast<const sl_f4 *>(p + 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = v[e] + a[e], v[4 + e] = v[4 + e] + b[e];
+            }
+            const float by = which == 0 ? A.s.scale : 1.0f;
+            const SlRows &to = which == 0 ? A.dk : A.dv;
+            *reinterpret_cast<sl_u4 *>(to.p + token * to.token + kv * to.head + octet * 16) =
+                sl_u4{sl_bf16_pair(v[0] * by, v[1] * by), sl_bf16_pair(v[2] * by, v[3] * by), sl_bf16_pair(v[4] * by, v[5] * by), sl_bf16_pair(v[6] * by, v[7] * by)};
+        }
     }
 }
 
@@ -682,6 +739,21 @@ bool few_tiles(int64_t rows, int64_t n, int64_t heads, int64_t other, int64_t ti
     const int64_t w = (rows / AT_ROWS + n) * heads, walk = other / n * times;
     return w <= (narrow ? 128 : 64) || w * (walk + 1400) < (narrow ? 900 : 400) * walk;
 }
+// Parts of a group's heads that the passes over keys take apart, joined in fp32: workgroups that walk past all of a group's queries are few and long
+// where key heads are few, and the longest walk is the pass.  From 512 workgroups of 128 keys on (two to a compute unit), and where no walk is long,
+// the join costs what it gives.  Backward, us, one slice / sliced: 8192 tokens, 20 heads of 128 on 5 1798 / 1248, 4096, 8 on 1 539 / 251, 512, 8 on 1
+// 71 / 47, 4 x 2048, 20 on 5 467 / 403; 2 x 512, 20 on 5 58 / 63, 8 x 1024, 16 heads of 64 on 4 99 / 121, 4 x 256, 16 on 2 34 / 41.
+enum { SLICED_BELOW = 512, SLICED_TO = 1024, LONG_WALK = 8192, HARDLY_ANY = 64, MOST_PART_ROWS = (SLICED_BELOW + SLICED_TO) * AT_ROWS };
+int64_t part_rows(int64_t tokens_q, int64_t heads) { return std::min<int64_t>(tokens_q * heads, MOST_PART_ROWS); }      // (of 2 x 128 floats)
+int slice_count(const SlSequences &s, int64_t kv_heads)
+{
+    const int64_t w = (s.tokens_k / AT_ROWS + s.n) * kv_heads;
+    if (w >= SLICED_BELOW || s.tokens_q == 0 || s.tokens_q / s.n * (int64_t)s.group < (w <= HARDLY_ANY ? LONG_WALK / 2 : LONG_WALK)) return 1;
+    int64_t slices = std::min<int64_t>(s.group, (SLICED_TO + w - 1) / w);
+    while (slices > 1 && slices * s.tokens_k * kv_heads > part_rows(s.tokens_q, s.heads)) --slices;      // (more keys than queries: what the room holds)
+    return (int)slices;
+}
+int64_t stats_floats(int64_t tokens_q, int64_t heads) { return (2 * tokens_q * heads + 2 + 3) / 4 * 4; }
 unsigned tile_count(int64_t tokens, int64_t n, bool few) { return (unsigned)(tokens / (few ? 32 : AT_ROWS) + n); }
 
 template <class Args>
@@ -726,7 +798,7 @@ int sl_attention(const sl_attention_shape *shape, const sl_heads *q, const sl_he
 size_t sl_attention_workspace_bytes(int64_t tokens_q, int64_t heads)
 {
     if (tokens_q < 1 || heads < 1 || tokens_q > AT_MOST_TOKENS || heads > AT_MOST_HEADS) return 0;
-    return sizeof(float) * (size_t)(2 * tokens_q * heads + 2);
+    return sizeof(float) * (size_t)(stats_floats(tokens_q, heads) + 256 * part_rows(tokens_q, heads));
 }
 
 int sl_attention_backward(const sl_attention_shape *shape, const sl_heads *q, const sl_heads *k, const sl_heads *v, const sl_heads *out,
@@ -760,10 +832,16 @@ int sl_attention_backward(const sl_attention_shape *shape, const sl_heads *q, co
             return rc;
     }
     if (!keys) return SL_OK;
-    const bool few = few_tiles(A.s.tokens_k, A.s.n, kv_heads, A.s.tokens_q, A.s.group, narrow);
+    A.slices = slice_count(A.s, kv_heads);
+    A.parts = A.stats + stats_floats(A.s.tokens_q, A.s.heads);
+    const bool few = few_tiles(A.s.tokens_k, A.s.n, kv_heads * A.slices, A.s.tokens_q, (A.s.group + A.slices - 1) / A.slices, narrow);
     A.s.tiles = tile_count(A.s.tokens_k, A.s.n, few);
-    if (few) return launch(narrow ? k_back_kv_few<64> : k_back_kv_few<128>, A, kv_heads, 8 * tile + 2048, st);
-    return launch(narrow ? k_back_kv<64> : k_back_kv<128>, A, kv_heads, 4 * tile + 512, st);
+    if (const int rc = few ? launch(narrow ? k_back_kv_few<64> : k_back_kv_few<128>, A, kv_heads * A.slices, 8 * tile + 2048, st)
+                           : launch(narrow ? k_back_kv<64> : k_back_kv<128>, A, kv_heads * A.slices, 4 * tile + 512, st))
+        return rc;
+    if (A.slices == 1) return SL_OK;
+    A.s.tiles = tile_count(A.s.tokens_k, A.s.n, false);
+    return launch(k_join_kv, A, kv_heads, 0, st);
 }
 
 }  // extern "C"

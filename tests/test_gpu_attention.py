@@ -277,6 +277,16 @@ def test_many_sequences_of_both_lengths(dim, causal):
     check(q, k, v, dout, qn, kn, causal, None)
 
 
+@pytest.mark.parametrize("qn,kn,count,heads,kv_heads,dim", [
+    ([700], [700], None, 8, 1, 128), ([1500, 20], [1500, 40], [1400, 33], 8, 1, 64), ([600], [1000], None, 8, 1, 72), ([520], [4000], None, 8, 1, 40),
+    ([1400], [1400], None, 9, 3, 128), ([2048], [2048], None, 64, 16, 128), ([0, 1100], [300, 1100], None, 16, 2, 64)])
+def test_few_key_heads_on_long_sequences(qn, kn, count, heads, kv_heads, dim):
+    """Gradients of keys and values whose group is walked past in parts, by workgroups of 32 keys and of 128; more keys than the parts have room for."""
+    first = 11
+    q, k, v, dout = tensors(first + sum(qn) + 3, first + sum(kn) + 3, heads, kv_heads, dim, seed=12)
+    check(q, k, v, dout, qn, kn, True, None, k_count=count, first=first, tail=3)
+
+
 @pytest.mark.parametrize("n", [63, 64, 65, 256, 257, 400])
 def test_numbers_of_sequences(n):
     """Lists that are ordered by work and lists that are too many for it."""
