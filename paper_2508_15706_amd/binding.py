@@ -216,12 +216,13 @@ def lib():
     return _lib
 
 
-def _stream_ptr(stream) -> Optional[int]:
+def _stream_ptr(stream, device: Optional[int] = None) -> Optional[int]:
+    """device: the current one, where the caller knows it."""
     if stream is None:
         # (the handle itself: the Stream object that torch.cuda.current_stream() makes costs 2.7 us a call, as much
         # as a third of a kernel launch, and a round on a short list makes several calls)
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # (not a public name: it may go)
-        return (raw(torch.cuda.current_device()) if raw else torch.cuda.current_stream().cuda_stream) or None
+        return (raw(torch.cuda.current_device() if device is None else device) if raw else torch.cuda.current_stream().cuda_stream) or None
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream or None
     return int(stream) or None
@@ -728,11 +729,12 @@ def _same(what: str, t: Optional[torch.Tensor], shape, dtype=None) -> None:
         raise ValueError(f"{what}: expected {tuple(shape)}{'' if dtype is None else ' of ' + str(dtype)}, got {tuple(t.shape)} of {t.dtype}")
 
 
-def _on_current_device(*tensors: Optional[torch.Tensor]) -> None:
+def _on_current_device(*tensors: Optional[torch.Tensor]) -> int:
     here = torch.cuda.current_device()
     for t in tensors:
         if t is not None and t.get_device() != here:
             raise ValueError(f"expected tensors on the current device ({here}), got one on {t.device}")
+    return here
 
 
 def _second(what: str, t: Optional[torch.Tensor], shape, dtype=None):
@@ -769,9 +771,9 @@ def sl_rms_norm(x: torch.Tensor, weight: torch.Tensor, y: Optional[torch.Tensor]
     rp, _, ldr = _second("residual", residual, x.shape)
     hp, ht, ldh = _second("h", h, x.shape, None if residual is None else residual.dtype)
     yp, yt, ldy = _second("y", y, x.shape)
-    _on_current_device(x, weight, y, residual, h, rstd, q, qt)
+    here = _on_current_device(x, weight, y, residual, h, rstd, q, qt)
     st = lib().sl_rms_norm(xp, xt, ldx, rp, ldr, hp, ht, ldh, _dev_ptr(weight), _type_of(weight), rows, cols, float(eps), yp, yt, ldy,
-                           _room("rstd", rstd, rows, torch.float32), _mx4_ptr(q, rows, cols), _mx4_ptr(qt, cols, rows), _stream_ptr(stream))
+                           _room("rstd", rstd, rows, torch.float32), _mx4_ptr(q, rows, cols), _mx4_ptr(qt, cols, rows), _stream_ptr(stream, here))
     if st:
         raise SparseLoCoError("sl_rms_norm", st)
 
@@ -786,11 +788,11 @@ def sl_rms_norm_backward(h: torch.Tensor, weight: torch.Tensor, rstd: torch.Tens
     gp, gt, ldg = _second("dy", dy, h.shape)
     op, ot, ldo = _second("dx", dx, h.shape)
     ip, _, ldi = _second("dh", dh, h.shape, dx.dtype)
-    _on_current_device(h, weight, rstd, dy, dx, dh, dw, workspace)
+    here = _on_current_device(h, weight, rstd, dy, dx, dh, dw, workspace)
     st = lib().sl_rms_norm_backward(hp, ht, ldh, _dev_ptr(weight), _type_of(weight), _room("rstd", rstd, rows, torch.float32), gp, gt, ldg,
                                     ip, ldi, op, ot, ldo, _dev_ptr(dw), int(accumulate), rows, cols,
                                     _room("workspace", workspace, 0 if dw is None else sl_rms_norm_workspace_bytes(rows, cols), torch.uint8),
-                                    _stream_ptr(stream))
+                                    _stream_ptr(stream, here))
     if st:
         raise SparseLoCoError("sl_rms_norm_backward", st)
 
@@ -827,9 +829,9 @@ def sl_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.T
     ends (k_start None: q_start); k_count: how many of a sequence's keys are used; scale None: dim ** -0.5; lse: (heads, tokens) fp32."""
     shape = _attention_shape(q, k, q_start, q_start if k_start is None else k_start, k_count, scale, causal)
     _same("lse", lse, (q.shape[1], q.shape[0]), torch.float32)
-    _on_current_device(q, k, v, out, q_start, k_start, k_count, lse)
+    here = _on_current_device(q, k, v, out, q_start, k_start, k_count, lse)
     st = lib().sl_attention(shape, _heads("q", q, q.shape), _heads("k", k, k.shape), _heads("v", v, k.shape), _heads("out", out, q.shape),
-                            _dev_ptr(lse), _stream_ptr(stream))
+                            _dev_ptr(lse), _stream_ptr(stream, here))
     if st:
         raise SparseLoCoError("sl_attention", st)
 
@@ -850,12 +852,12 @@ def sl_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out
     """dq, dk, dv from dout and what sl_attention was given and left."""
     shape = _attention_shape(q, k, q_start, q_start if k_start is None else k_start, k_count, scale, causal)
     _same("lse", lse, (q.shape[1], q.shape[0]), torch.float32)
-    _on_current_device(q, k, v, out, lse, dout, dq, dk, dv, q_start, k_start, k_count, workspace)
+    here = _on_current_device(q, k, v, out, lse, dout, dq, dk, dv, q_start, k_start, k_count, workspace)
     st = lib().sl_attention_backward(shape, _heads("q", q, q.shape), _heads("k", k, k.shape), _heads("v", v, k.shape),
                                      _heads("out", out, q.shape), _dev_ptr(lse), _heads("dout", dout, q.shape), _heads("dq", dq, q.shape),
                                      _heads("dk", dk, k.shape), _heads("dv", dv, k.shape),
                                      _room("workspace", workspace, sl_attention_workspace_bytes(q.shape[0], q.shape[1]), torch.uint8),
-                                     _stream_ptr(stream))
+                                     _stream_ptr(stream, here))
     if st:
         raise SparseLoCoError("sl_attention_backward", st)
 
@@ -874,10 +876,10 @@ def sl_attention_token(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: t
                        stream=None) -> None:
     """One query per sequence: q, out (sequences, heads, dim); k, v (tokens, kv_heads, dim), the caches of all sequences."""
     shape = _attention_shape(q, k, None, k_start, k_count, scale, False)
-    _on_current_device(q, k, v, out, k_start, k_count, workspace)
+    here = _on_current_device(q, k, v, out, k_start, k_count, workspace)
     st = lib().sl_attention_token(shape, _heads("q", q, q.shape), _heads("k", k, k.shape), _heads("v", v, k.shape), _heads("out", out, q.shape),
                                   _room("workspace", workspace, sl_attention_token_workspace_bytes(q.shape[0], k.shape[0], q.shape[1], k.shape[1],
-                                                                                                  q.shape[2]), torch.uint8), _stream_ptr(stream))
+                                                                                                  q.shape[2]), torch.uint8), _stream_ptr(stream, here))
     if st:
         raise SparseLoCoError("sl_attention_token", st)
 
@@ -915,9 +917,9 @@ def sl_token_loss(logits: torch.Tensor, targets: torch.Tensor, weights: Optional
             _same(what, getattr(policy, what), (rows,), torch.float32)
         _on_current_device(policy.old_logp, policy.advantage, policy.ref_logp)
         pol = SlPolicy(_dev_ptr(policy.old_logp), _dev_ptr(policy.advantage), _dev_ptr(policy.ref_logp), policy.clip_low, policy.clip_high, policy.kl)
-    _on_current_device(logits, targets, weights, loss, logp, dlogits, workspace)
+    here = _on_current_device(logits, targets, weights, loss, logp, dlogits, workspace)
     st = lib().sl_token_loss(p, typ, ld, rows, vocab, _dev_ptr(targets), _dev_ptr(weights), pol, _room("loss", loss, 1, torch.float32), _dev_ptr(logp),
                              dp, ldd, _room("workspace", workspace, 0 if loss is None else sl_token_loss_workspace_bytes(rows), torch.uint8),
-                             _stream_ptr(stream))
+                             _stream_ptr(stream, here))
     if st:
         raise SparseLoCoError("sl_token_loss", st)
