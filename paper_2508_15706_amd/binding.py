@@ -816,7 +816,9 @@ def _starts(what: str, t: Optional[torch.Tensor], n: Optional[int] = None) -> Op
 
 def _attention_shape(q, k, q_start, k_start, k_count, scale, causal) -> SlAttentionShape:
     tokens_q, heads, dim = q.shape
-    tokens_k, kv_heads, _ = k.shape
+    tokens_k, kv_heads, width = k.shape
+    if width != dim:                                  # (the kernels take a row's width from the queries)
+        _same("k", k, (tokens_k, kv_heads, dim))
     n = k_start.numel() - 1
     return SlAttentionShape(n, tokens_q, tokens_k, heads, kv_heads, dim, int(causal), dim ** -0.5 if scale is None else float(scale),
                             _starts("q_start", q_start, n + 1), _starts("k_start", k_start), _starts("k_count", k_count, n))
