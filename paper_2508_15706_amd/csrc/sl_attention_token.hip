@@ -1,12 +1,8 @@
 // Attention of one new token per sequence over its cache.
-#include <algorithm>
-
 #include "sl_attention.h"
+#include "sl_attention_rules.h"
 
 namespace {
-
-// Keys of a part: one wave's work.
-enum { LEAST_PART = 32, LONGEST_PART = 512, MOST_WAVES = 1280 };
 
 struct TokenArgs {
     SlSequences s;
@@ -134,19 +130,6 @@ int check_launch()
     return SL_ERR_HIP;
 }
 
-// Parts are as short as leaves about MOST_WAVES of them: for one sequence their number counts, for many their evenness.
-unsigned part_size(int64_t tokens, int64_t units)
-{
-    unsigned part = LEAST_PART;
-    while (part < LONGEST_PART && tokens / part * units > MOST_WAVES) part *= 2;
-    return part;
-}
-int64_t most_parts(int64_t sequences, int64_t tokens, int64_t units)
-{
-    return std::min(tokens / LEAST_PART, std::max<int64_t>(MOST_WAVES / units, tokens / LONGEST_PART)) + sequences;
-}
-int64_t unit_count(int64_t heads, int64_t kv_heads) { return kv_heads * ((heads / kv_heads + 31) / 32); }
-
 }  // namespace
 
 extern "C" {
@@ -156,7 +139,7 @@ size_t sl_attention_token_workspace_bytes(int64_t sequences, int64_t tokens_k, i
     if (sequences < 1 || sequences > AT_MOST_SEQUENCES || tokens_k < 0 || tokens_k > AT_MOST_TOKENS || heads < 1 || heads > AT_MOST_HEADS ||
         kv_heads < 1 || heads % kv_heads != 0 || head_dim < 8 || head_dim > 128 || head_dim % 8 != 0)
         return 0;
-    return sizeof(float) * (size_t)(most_parts(sequences, tokens_k, unit_count(heads, kv_heads)) * heads * (head_dim + 2));
+    return sizeof(float) * (size_t)(sl_token_room(sl_token_most_parts(sequences, tokens_k, sl_token_units(heads, kv_heads)), heads, head_dim).floats);
 }
 
 int sl_attention_token(const sl_attention_shape *shape, const sl_heads *q, const sl_heads *k, const sl_heads *v, const sl_heads *out, void *workspace,
@@ -172,12 +155,13 @@ int sl_attention_token(const sl_attention_shape *shape, const sl_heads *q, const
     const void *in[4] = {q->data, keys ? k->data : nullptr, keys ? v->data : nullptr, workspace};
     for (const void *p : in)
         if (p == out->data) return SL_ERR_INVALID_ARG;
-    const int64_t units = unit_count(shape->heads, shape->kv_heads);
-    A.part = part_size(A.s.tokens_k, units);
+    const int64_t units = sl_token_units(shape->heads, shape->kv_heads);
+    A.part = sl_token_part(A.s.tokens_k, units);
     A.s.tiles = (unsigned)A.s.tokens_k / A.part + (unsigned)A.s.n;
     if ((int64_t)(A.s.tiles + 7) / 8 * 8 * units >= (int64_t)1 << 24 || (int64_t)A.s.n * A.s.heads >= (int64_t)1 << 25) return SL_ERR_INVALID_ARG;
-    A.stats = static_cast<float *>(workspace);
-    A.parts = A.stats + 2 * (int64_t)A.s.tiles * A.s.heads;
+    const SlTokenRoom room = sl_token_room(A.s.tiles, A.s.heads, shape->head_dim);
+    A.parts = static_cast<float *>(workspace) + room.values;
+    A.stats = static_cast<float *>(workspace) + room.stats;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (keys) {
         const bool narrow = A.s.octets <= 8;
