@@ -515,6 +515,7 @@ int sl_rms_norm_backward(const void *h, int h_type, int64_t ldh, const void *wei
  * weights   in, device, fp32, or NULL = 1.  A token that does not count or has a weight of 0 adds nothing to the loss, whatever its
  *           logits and its policy inputs are, and its gradient is zero; its logp is 0 where it does not count
  * loss      out, device, float[1], or NULL;  logp: out, device, float[rows], or NULL (both of the logits given, before any update)
+ *           logp may be one of the arrays of a value per row that are read (weights, the policy's)
  * dlogits   out, device, of `type`, rows x vocab, row i at element i*ldd, or NULL; may be logits itself (with ldd = ld)
  * workspace device, sl_token_loss_workspace_bytes(rows), 16-byte aligned; may be NULL where loss is
  * 0 <= clip_low <= 1, clip_high >= 0, kl >= 0, finite; ref_logp may be NULL where kl is 0.  rows <= 2^21, 1 <= vocab <= 2^24.

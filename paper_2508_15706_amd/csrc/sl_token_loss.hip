@@ -208,7 +208,6 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, OCT == 13 ? 4 :
                 for (int i = 1; i < WAVES; ++i) sum = sum + sums[i];
             }
             const double logp = ((double)zt - (double)m) - log(sum);
-            if (A.logp) A.logp[row] = (float)logp;
             if (counts) {
                 double loss, d;
                 token_loss(A, row, logp, loss, d);
@@ -216,6 +215,7 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES, OCT == 13 ? 4 :
                 slope = (float)((double)weight * d), share = (float)(-((double)weight * d) / sum);
                 if constexpr (WAVES > 1) told[0] = slope, told[1] = share;
             }
+            if (A.logp) A.logp[row] = (float)logp;        // (it may lie where the row's policy inputs did)
         }
         if (A.dlogits && counts) {
             if constexpr (WAVES > 1) {
