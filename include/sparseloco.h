@@ -555,9 +555,12 @@ typedef struct {                               /* element (t, h, d) at data + t*
 int sl_attention(const sl_attention_shape *shape, const sl_heads *q, const sl_heads *k, const sl_heads *v, const sl_heads *out, float *lse,
                  void *stream);
 /* Gradients from that of out: dq like q, dk and dv like k and v, each summed over the heads that share it, in a fixed order.
- * out, lse   in, as sl_attention left them;  workspace: device, sl_attention_workspace_bytes (some 200 MB at most beyond 8 bytes a query and head:
- *            room for parts of a group's sums), 16-byte aligned; that of the largest call serves smaller ones */
+ * out, lse   in, as sl_attention left them
+ * workspace  device, 16-byte aligned, sl_attention_group_workspace_bytes for the call's heads and width: 8 bytes a query and head and, where heads share a key
+ *            head, room for parts of a group's sums, some 200 MB at most; that for the most queries serves fewer.  sl_attention_workspace_bytes is
+ *            enough for any kv_heads and head_dim */
 size_t sl_attention_workspace_bytes(int64_t tokens_q, int64_t heads);
+size_t sl_attention_group_workspace_bytes(int64_t tokens_q, int heads, int kv_heads, int head_dim);
 int sl_attention_backward(const sl_attention_shape *shape, const sl_heads *q, const sl_heads *k, const sl_heads *v, const sl_heads *out,
                           const float *lse, const sl_heads *dout, const sl_heads *dq, const sl_heads *dk, const sl_heads *dv, void *workspace,
                           void *stream);

@@ -40,7 +40,7 @@ EXPORTS = [
     "sl_adamw_step", "sl_adamw_step8", "sl_adamw_state_values",
     "sl_mx4_bytes", "sl_mx4_quantize", "sl_mx4_dequantize", "sl_mx4_workspace_bytes", "sl_mx4_product", "sl_mx4_linear",
     "sl_rms_norm", "sl_rms_norm_workspace_bytes", "sl_rms_norm_backward",
-    "sl_attention", "sl_attention_workspace_bytes", "sl_attention_backward",
+    "sl_attention", "sl_attention_workspace_bytes", "sl_attention_group_workspace_bytes", "sl_attention_backward",
     "sl_attention_token_workspace_bytes", "sl_attention_token",
     "sl_token_loss_workspace_bytes", "sl_token_loss",
 ]
@@ -198,6 +198,8 @@ def lib():
         L.sl_attention.argtypes = [ps, ph, ph, ph, ph, vp, vp]
         L.sl_attention_workspace_bytes.restype = sz
         L.sl_attention_workspace_bytes.argtypes = [i64, i64]
+        L.sl_attention_group_workspace_bytes.restype = sz
+        L.sl_attention_group_workspace_bytes.argtypes = [i64, i32, i32, i32]
         L.sl_attention_backward.restype = i32
         L.sl_attention_backward.argtypes = [ps, ph, ph, ph, ph, vp, ph, ph, ph, ph, vp, vp]
         L.sl_attention_token_workspace_bytes.restype = sz
@@ -843,8 +845,15 @@ def sl_attention_workspace_bytes(tokens: int, heads: int) -> int:
     return int(lib().sl_attention_workspace_bytes(int(tokens), int(heads)))
 
 
-def alloc_attention_workspace(tokens: int, heads: int, device="cuda") -> torch.Tensor:
-    return torch.empty(max(16, sl_attention_workspace_bytes(tokens, heads)), dtype=torch.uint8, device=device)
+@functools.lru_cache(maxsize=4096)
+def sl_attention_group_workspace_bytes(tokens: int, heads: int, kv_heads: int, dim: int) -> int:
+    return int(lib().sl_attention_group_workspace_bytes(int(tokens), int(heads), int(kv_heads), int(dim)))
+
+
+def alloc_attention_workspace(tokens: int, heads: int, device="cuda", kv_heads: Optional[int] = None, dim: int = 128) -> torch.Tensor:
+    """kv_heads None: for any number of key heads and any width (200 MB more than it takes where every head has a key head of its own)."""
+    size = sl_attention_workspace_bytes(tokens, heads) if kv_heads is None else sl_attention_group_workspace_bytes(tokens, heads, kv_heads, dim)
+    return torch.empty(max(16, size), dtype=torch.uint8, device=device)
 
 
 def sl_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor, dout: torch.Tensor,
@@ -858,7 +867,7 @@ def sl_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out
     st = lib().sl_attention_backward(shape, _heads("q", q, q.shape), _heads("k", k, k.shape), _heads("v", v, k.shape),
                                      _heads("out", out, q.shape), _dev_ptr(lse), _heads("dout", dout, q.shape), _heads("dq", dq, q.shape),
                                      _heads("dk", dk, k.shape), _heads("dv", dv, k.shape),
-                                     _room("workspace", workspace, sl_attention_workspace_bytes(q.shape[0], q.shape[1]), torch.uint8),
+                                     _room("workspace", workspace, sl_attention_group_workspace_bytes(q.shape[0], q.shape[1], k.shape[1], q.shape[2]), torch.uint8),
                                      _stream_ptr(stream, here))
     if st:
         raise SparseLoCoError("sl_attention_backward", st)

@@ -56,7 +56,7 @@ class BlockModel:
         self.mixed, self.lse, self.added = b16(n, heads, dim), f32(heads, n), b16(n, d)
         self.logits, self.loss, self.logp = b16(n, vocab), f32(1), f32(n)
         self.dh = f32(n, d)
-        self.attend_ws, self.loss_ws = sl.alloc_attention_workspace(n, heads), sl.alloc_token_loss_workspace(n)
+        self.attend_ws, self.loss_ws = sl.alloc_attention_workspace(n, heads, kv_heads=kv_heads, dim=dim), sl.alloc_token_loss_workspace(n)
         self.rms_ws = sl.alloc_rms_norm_workspace(n, d)
         self.error = torch.zeros(off, device="cuda")
         self.step = 0

@@ -8,6 +8,7 @@
 //   8 + 4 h + {0..3}, and the other operand is read in the same order - transposed, four rows at a time, out of LDS.  So no
 //   probability ever moves between lanes.
 #pragma once
+#include "sl_attention_rules.h"
 #include "sl_dma.h"
 #include "sl_mx4.h"
 
@@ -19,8 +20,8 @@
 typedef float sl_f16 __attribute__((ext_vector_type(16)));
 typedef __bf16 sl_b8 __attribute__((ext_vector_type(8)));
 
-// Rows of a workgroup, 32 to each of its waves; rows of the other side in a stage of LDS, and in a short one.
-enum { AT_ROWS = 128, AT_TILE = 64, AT_STAGE = 32 };
+// Rows of the other side in a stage of LDS, and in a short one.
+enum { AT_TILE = 64, AT_STAGE = 32 };
 
 struct SlRows {                  // a tensor of tokens x heads x dim; strides in bytes
     unsigned char *p;

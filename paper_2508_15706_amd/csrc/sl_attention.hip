@@ -739,21 +739,6 @@ bool few_tiles(int64_t rows, int64_t n, int64_t heads, int64_t other, int64_t ti
     const int64_t w = (rows / AT_ROWS + n) * heads, walk = other / n * times;
     return w <= (narrow ? 128 : 64) || w * (walk + 1400) < (narrow ? 900 : 400) * walk;
 }
-// Parts of a group's heads that the passes over keys take apart, joined in fp32: workgroups that walk past all of a group's queries are few and long
-// where key heads are few, and the longest walk is the pass.  From 512 workgroups of 128 keys on (two to a compute unit), and where no walk is long,
-// the join costs what it gives.  Backward, us, one slice / sliced: 8192 tokens, 20 heads of 128 on 5 1798 / 1248, 4096, 8 on 1 539 / 251, 512, 8 on 1
-// 71 / 47, 4 x 2048, 20 on 5 467 / 403; 2 x 512, 20 on 5 58 / 63, 8 x 1024, 16 heads of 64 on 4 99 / 121, 4 x 256, 16 on 2 34 / 41.
-enum { SLICED_BELOW = 512, SLICED_TO = 1024, LONG_WALK = 8192, HARDLY_ANY = 64, MOST_PART_ROWS = (SLICED_BELOW + SLICED_TO) * AT_ROWS };
-int64_t part_rows(int64_t tokens_q, int64_t heads) { return std::min<int64_t>(tokens_q * heads, MOST_PART_ROWS); }      // (of 2 x 128 floats)
-int slice_count(const SlSequences &s, int64_t kv_heads)
-{
-    const int64_t w = (s.tokens_k / AT_ROWS + s.n) * kv_heads;
-    if (w >= SLICED_BELOW || s.tokens_q == 0 || s.tokens_q / s.n * (int64_t)s.group < (w <= HARDLY_ANY ? LONG_WALK / 2 : LONG_WALK)) return 1;
-    int64_t slices = std::min<int64_t>(s.group, (SLICED_TO + w - 1) / w);
-    while (slices > 1 && slices * s.tokens_k * kv_heads > part_rows(s.tokens_q, s.heads)) --slices;      // (more keys than queries: what the room holds)
-    return (int)slices;
-}
-int64_t stats_floats(int64_t tokens_q, int64_t heads) { return (2 * tokens_q * heads + 2 + 3) / 4 * 4; }
 unsigned tile_count(int64_t tokens, int64_t n, bool few) { return (unsigned)(tokens / (few ? 32 : AT_ROWS) + n); }
 
 template <class Args>
@@ -795,10 +780,18 @@ int sl_attention(const sl_attention_shape *shape, const sl_heads *q, const sl_he
     return launch(narrow ? k_attend<64> : k_attend<128>, A, A.s.heads, 4 * tile, st);
 }
 
+size_t sl_attention_group_workspace_bytes(int64_t tokens_q, int heads, int kv_heads, int head_dim)
+{
+    if (tokens_q < 1 || tokens_q > AT_MOST_TOKENS || heads < 1 || heads > AT_MOST_HEADS || kv_heads < 1 || heads % kv_heads != 0 || head_dim < 8 ||
+        head_dim > 128 || head_dim % 8 != 0)
+        return 0;
+    return sizeof(float) * (size_t)sl_back_room(tokens_q, heads, kv_heads, head_dim);
+}
+
 size_t sl_attention_workspace_bytes(int64_t tokens_q, int64_t heads)
 {
     if (tokens_q < 1 || heads < 1 || tokens_q > AT_MOST_TOKENS || heads > AT_MOST_HEADS) return 0;
-    return sizeof(float) * (size_t)(stats_floats(tokens_q, heads) + 256 * part_rows(tokens_q, heads));
+    return sizeof(float) * (size_t)sl_back_room(tokens_q, heads, 1, 128);
 }
 
 int sl_attention_backward(const sl_attention_shape *shape, const sl_heads *q, const sl_heads *k, const sl_heads *v, const sl_heads *out,
@@ -832,8 +825,8 @@ int sl_attention_backward(const sl_attention_shape *shape, const sl_heads *q, co
             return rc;
     }
     if (!keys) return SL_OK;
-    A.slices = slice_count(A.s, kv_heads);
-    A.parts = A.stats + stats_floats(A.s.tokens_q, A.s.heads);
+    A.slices = sl_back_slices(A.s.tokens_q, A.s.tokens_k, A.s.n, A.s.heads, kv_heads);
+    A.parts = A.stats + sl_back_stats(A.s.tokens_q, A.s.heads);
     const bool few = few_tiles(A.s.tokens_k, A.s.n, kv_heads * A.slices, A.s.tokens_q, (A.s.group + A.slices - 1) / A.slices, narrow);
     A.s.tiles = tile_count(A.s.tokens_k, A.s.n, few);
     if (const int rc = few ? launch(narrow ? k_back_kv_few<64> : k_back_kv_few<128>, A, kv_heads * A.slices, 8 * tile + 2048, st)

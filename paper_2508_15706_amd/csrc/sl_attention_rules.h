@@ -4,6 +4,36 @@
 #include <stddef.h>
 #include <stdint.h>
 
+// Rows of a workgroup, 32 to each of its waves.
+enum { AT_ROWS = 128 };
+
+// ---- backward ----
+
+// Parts of a group's heads that the passes over keys take apart, joined in fp32: workgroups that walk past all of a group's queries are few and long
+// where key heads are few, and the longest walk is the pass.  From 512 workgroups of 128 keys on (two to a compute unit), and where no walk is long,
+// the join costs what it gives.  Backward, us, one slice / sliced: 8192 tokens, 20 heads of 128 on 5 1798 / 1248, 4096, 8 on 1 539 / 251, 512, 8 on 1
+// 71 / 47, 4 x 2048, 20 on 5 467 / 403; 2 x 512, 20 on 5 58 / 63, 8 x 1024, 16 heads of 64 on 4 99 / 121, 4 x 256, 16 on 2 34 / 41.
+enum { AT_SLICED_BELOW = 512, AT_SLICED_TO = 1024, AT_LONG_WALK = 8192, AT_HARDLY_ANY = 64, AT_MOST_PART_ROWS = (AT_SLICED_BELOW + AT_SLICED_TO) * AT_ROWS };
+// Rows of dk and of dv that the parts of any call with so many queries have; none where no heads share a key head.
+inline int64_t sl_back_part_rows(int64_t tokens_q, int64_t heads, int64_t kv_heads)
+{
+    return heads == kv_heads ? 0 : std::min<int64_t>(tokens_q * heads, AT_MOST_PART_ROWS);
+}
+inline int sl_back_slices(int64_t tokens_q, int64_t tokens_k, int64_t sequences, int64_t heads, int64_t kv_heads)
+{
+    const int64_t w = (tokens_k / AT_ROWS + sequences) * kv_heads, group = heads / kv_heads;
+    if (w >= AT_SLICED_BELOW || tokens_q == 0 || tokens_q / sequences * group < (w <= AT_HARDLY_ANY ? AT_LONG_WALK / 2 : AT_LONG_WALK)) return 1;
+    int64_t slices = std::min<int64_t>(group, (AT_SLICED_TO + w - 1) / w);
+    while (slices > 1 && slices * tokens_k * kv_heads > sl_back_part_rows(tokens_q, heads, kv_heads)) --slices;      // (more keys than queries: what the room holds)
+    return (int)slices;
+}
+// A workspace, in floats: the queries' statistics and what stands for no query, then the parts.
+inline int64_t sl_back_stats(int64_t tokens_q, int64_t heads) { return (2 * tokens_q * heads + 2 + 3) / 4 * 4; }
+inline int64_t sl_back_room(int64_t tokens_q, int64_t heads, int64_t kv_heads, int64_t dim)
+{
+    return sl_back_stats(tokens_q, heads) + 2 * dim * sl_back_part_rows(tokens_q, heads, kv_heads);
+}
+
 // ---- single tokens ----
 
 // Keys of a part: one wave's work.

@@ -1,6 +1,5 @@
 // Attention of one new token per sequence over its cache.
 #include "sl_attention.h"
-#include "sl_attention_rules.h"
 
 namespace {
 

@@ -26,9 +26,34 @@ static void tokens()
                 }
 }
 
+static void backward()
+{
+    const int heads[][2] = {{1, 1}, {16, 16}, {2, 1}, {8, 1}, {20, 5}, {64, 16}, {16, 2}, {9, 3}, {4096, 1}, {65536, 4}};
+    for (const auto &h : heads)
+        for (const int64_t n : {1, 2, 7, 100, 5000}) {
+            int64_t before[3] = {0, 0, 0};
+            for (int64_t q = 1; q < 2000000; q += q < 300 ? 1 : q / 13) {
+                const int64_t dims[3] = {8, 72, 128};
+                for (int d = 0; d < 3; ++d) {
+                    const int64_t room = sl_back_room(q, h[0], h[1], dims[d]);
+                    if (sl_back_stats(q, h[0]) % 4 != 0 || sl_back_stats(q, h[0]) < 2 * q * h[0] + 2) fail("statistics", q, n, h[0], h[1]);
+                    if (room < before[d] || room > sl_back_room(q, h[0], 1, 128)) fail("fewer queries, or any heads", q, n, h[0], h[1]);
+                    if (h[0] == h[1] && room != sl_back_stats(q, h[0])) fail("room for parts that there are none of", q, n, h[0], h[1]);
+                    before[d] = room;
+                    for (const int64_t k : {q / 50, q / 2, q, 2 * q, 9 * q, (int64_t)1 << 20}) {
+                        const int64_t slices = sl_back_slices(q, k, n, h[0], h[1]);
+                        if (slices < 1 || slices > h[0] / h[1]) fail("slices", q, k, h[0], h[1]);
+                        if (slices > 1 && sl_back_stats(q, h[0]) + slices * 2 * k * h[1] * dims[d] > room) fail("parts", q, k, h[0], h[1]);
+                    }
+                }
+            }
+        }
+}
+
 int main()
 {
     tokens();
+    backward();
     if (failures == 0) std::puts("ok");
     return failures != 0;
 }

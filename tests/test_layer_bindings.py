@@ -16,3 +16,17 @@ def test_keys_as_wide_as_queries():
                      lambda: sl.sl_attention_token(q[:1], k, k.clone(), q[:1].clone(), s)):
             with pytest.raises(ValueError, match="k: expected"):
                 call()
+
+
+def test_workspaces_of_the_backward_pass():
+    """Where every head has a key head of its own there are statistics alone; narrow heads have narrow parts; any heads' room is enough for all."""
+    from paper_2508_15706_amd import binding as sl
+    size = sl.sl_attention_group_workspace_bytes
+    assert size(16384, 16, 16, 128) == 8 * 16384 * 16 + 16
+    assert size(8192, 20, 5, 64) - (8 * 8192 * 20 + 16) == 2 * 64 * 4 * 8192 * 20
+    for tokens, heads in ((1, 1), (33, 5), (8192, 20), (100000, 64)):
+        every = sl.sl_attention_workspace_bytes(tokens, heads)
+        for kv_heads in (1, heads):
+            for dim in (8, 40, 128):
+                assert 0 < size(tokens, heads, kv_heads, dim) <= every
+    assert [size(*bad) for bad in ((0, 4, 2, 64), (2**30 + 1, 4, 2, 64), (9, 4, 3, 64), (9, 4, 0, 64), (9, 0, 1, 64), (9, 4, 2, 60), (9, 4, 2, 136), (9, 2**17, 1, 8))] == [0] * 8
