@@ -86,8 +86,8 @@ class BlockModel:
         sl.sl_mx4_product(L["head"].x, L["head"].w, self.logits, self.d, L["head"].ws)
         sl.sl_token_loss(self.logits, targets, weights, self.loss, logp=self.logp, dlogits=self.logits, workspace=self.loss_ws)
 
-    def backward(self, tokens: torch.Tensor) -> None:
-        """Gradients of all parameters from what forward left."""
+    def backward_to_embeddings(self) -> None:
+        """Gradients of the layers' parameters, and of the tokens' embeddings in dh, from what forward left: nothing that sorts, so that a graph may hold it."""
         L, g = self.layers, self.grad
         self.dy2 = L["head"].backward(self.logits, self.view(g, "head"))
         sl.sl_rms_norm_backward(self.h1, self.view(self.theta, "norm2"), self.rstd2, self.dy2, self.dh, dw=self.view(g, "norm2"), workspace=self.rms_ws)
@@ -97,9 +97,16 @@ class BlockModel:
         sl.sl_attention_backward(q, k, v, self.mixed, self.lse, self.dmixed, dq, dk, dv, self.starts, workspace=self.attend_ws)
         self.dy1 = L["qkv"].backward(self.dqkv.view(self.tokens, -1), self.view(g, "qkv"))
         sl.sl_rms_norm_backward(self.h0, self.view(self.theta, "norm1"), self.rstd1, self.dy1, self.dh, dh=self.dh, dw=self.view(g, "norm1"), workspace=self.rms_ws)
-        embed = self.view(g, "embed")
+
+    def embedding_gradient(self, tokens: torch.Tensor) -> None:
+        embed = self.view(self.grad, "embed")
         embed.zero_()
         embed.index_put_((tokens,), self.dh, accumulate=True)
+
+    def backward(self, tokens: torch.Tensor) -> None:
+        """Gradients of all parameters from what forward left."""
+        self.backward_to_embeddings()
+        self.embedding_gradient(tokens)
 
     def update(self, lr: float, seed: int) -> None:
         sl.sl_grad_norm(self.opt, self.grad, 1.0, self.norm, self.norm_ws)
