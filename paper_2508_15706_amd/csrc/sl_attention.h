@@ -265,8 +265,8 @@ SL_DEV void sl_reads_ahead()
     __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
 }
 
-// Eight values of a score tile as the operand of the next product: rounded to bf16, which the matrix unit takes (half a step is
-// 2^-9 of a probability, random from one key to the next).
+// Eight values of a score tile as the operand of the next product: rounded to bf16, which the matrix unit takes (off by half a step at most,
+// 2^-8 of a probability, random from one key to the next).
 SL_DEV sl_b8 sl_operand(const sl_f16 &s, int g)
 {
     const sl_u4 w = g == 0 ? sl_u4{sl_bf16_pair(s[0], s[1]), sl_bf16_pair(s[2], s[3]), sl_bf16_pair(s[4], s[5]), sl_bf16_pair(s[6], s[7])}

@@ -33,10 +33,12 @@ struct BackArgs {
 
 // 128 queries of one head, 32 to a wave, over 64 keys at a time, two stages of LDS; the softmax in one pass, as in SlRunning (whose 32 keys
 // would leave the matrix unit one chain of products; here are two).  Two workgroups to a compute unit: 32 products of 32 cycles a wave and
-// 64 keys stand against about 1000 cycles of exponentials, sums and maxima, and the one's run beside the other's.
-// 8192 tokens, 20 heads of 128 on 5: 353 us, 0.97 PFLOP/s at 2.0 GHz; 8 x 2048 tokens, 16 heads: 175 us, 0.79 - the same loop on constant operands
-// in LDS, without masks, starts and ends: 1630 ns for 64 keys of two waves at 2.4 GHz, here 2170.  Tried and not kept: the next tile's scores beside this
-// one's exponentials in the same wave (111 registers spilled, 704 us), priorities of waves around products or exponentials (the same time).
+// 64 keys stand against about 900 cycles of exponentials, sums and maxima, of which less than half runs beside the other's products, since
+// nothing keeps the two out of phase.  The same loop on constant operands, without masks, starts and ends, at 2.4 GHz, 64 keys of two waves:
+// products alone 1005 ns, all but the reads of LDS 1440, all of it 1630; here 2170 at 2.0 GHz.
+// 8192 tokens, 20 heads of 128 on 5: 349 us, 0.98 PFLOP/s, the matrix unit busy 45 % of the time, the vector unit 42, LDS 23; 8 x 2048 tokens,
+// 16 heads: 175 us, 0.79.  Tried and not kept: the next tile's scores beside this one's exponentials in the same wave (111 registers spilled,
+// 704 us), priorities of waves around products or exponentials (the same time).
 template <int D>
 __global__ void __launch_bounds__(256, 2) k_attend(AttendArgs A)
 {
@@ -215,7 +217,7 @@ __global__ void __launch_bounds__(256, 1) k_attend_few(AttendArgs A)
 // ---- backward ----
 
 // dq: queries to lanes as in the forward pass; S and dP of 32 keys at a time.  It also leaves what the pass over keys needs of a query.
-// Three products where the pass over keys has four; 8 x 2048 tokens, 16 heads of 128: 232 us, 0.89 PFLOP/s.  (dq from that pass would need
+// Three products where the pass over keys has four; 8 x 2048 tokens, 16 heads of 128: 230 us, 0.90 PFLOP/s.  (dq from that pass would need
 // sums over workgroups, in memory or in an order that changes.)
 // sum dout out is that of P dP, too: for queries that see few keys, whose dP - sum dout out is small beside its terms, it is taken from there,
 // in a pass over the keys in front.  From out, which is rounded, it moves the dS of all of a query's keys the same way, by its own
@@ -481,8 +483,8 @@ SL_DEV void back_scores(sl_f16 &s, sl_f16 &dp, const float *stats, int from, flo
 
 // dk and dv: 128 keys of one key head, 32 to a wave, over all queries of the heads that share it, 32 at a time; the sums over the heads are
 // made in registers, in their order.  A wave holds its keys in registers and its values in LDS, so that two workgroups fit a compute unit
-// and one's exponentials run beside the other's products: 8 x 2048 tokens, 16 heads of 128, 320 us, 0.86 PFLOP/s (keys and values in registers, one
-// workgroup to a compute unit, 412).
+// and some of one's exponentials run beside the other's products: 8 x 2048 tokens, 16 heads of 128, 300 to 320 us, 0.86 to 0.92 PFLOP/s, the
+// matrix unit busy 45 % of the time, the vector unit 38, LDS 34 (keys and values in registers, one workgroup to a compute unit, 412 us).
 template <int D>
 __global__ void __launch_bounds__(256, 2) k_back_kv(BackArgs A)
 {

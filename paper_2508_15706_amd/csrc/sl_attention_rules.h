@@ -11,8 +11,8 @@ enum { AT_ROWS = 128 };
 
 // Parts of a group's heads that the passes over keys take apart, joined in fp32: workgroups that walk past all of a group's queries are few and long
 // where key heads are few, and the longest walk is the pass.  From 512 workgroups of 128 keys on (two to a compute unit), and where no walk is long,
-// the join costs what it gives.  Backward, us, one slice / sliced: 8192 tokens, 20 heads of 128 on 5 1798 / 1248, 4096, 8 on 1 539 / 251, 512, 8 on 1
-// 71 / 47, 4 x 2048, 20 on 5 467 / 403; 2 x 512, 20 on 5 58 / 63, 8 x 1024, 16 heads of 64 on 4 99 / 121, 4 x 256, 16 on 2 34 / 41.
+// the join costs what it gives.  Backward, us, one slice / sliced: 8192 tokens, 20 heads of 128 on 5 1775 / 1182, 4096, 8 on 1 543 / 257, 512, 8 on 1
+// 72 / 47, 4 x 2048, 20 on 5 486 / 400; 2 x 512, 20 on 5 58 / 63, 8 x 1024, 16 heads of 64 on 4 99 / 121, 4 x 256, 16 on 2 34 / 41.
 enum { AT_SLICED_BELOW = 512, AT_SLICED_TO = 1024, AT_LONG_WALK = 8192, AT_HARDLY_ANY = 64, AT_MOST_PART_ROWS = (AT_SLICED_BELOW + AT_SLICED_TO) * AT_ROWS };
 // Rows of dk and of dv that the parts of any call with so many queries have; none where no heads share a key head.
 inline int64_t sl_back_part_rows(int64_t tokens_q, int64_t heads, int64_t kv_heads)
