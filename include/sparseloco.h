@@ -564,8 +564,8 @@ size_t sl_attention_group_workspace_bytes(int64_t tokens_q, int heads, int kv_he
 int sl_attention_backward(const sl_attention_shape *shape, const sl_heads *q, const sl_heads *k, const sl_heads *v, const sl_heads *out,
                           const float *lse, const sl_heads *dout, const sl_heads *dq, const sl_heads *dk, const sl_heads *dv, void *workspace,
                           void *stream);
-/* One new token per sequence (generation): query s is sequence s's and sees all of its keys; tokens_q = sequences, q_start and causal
- * are not looked at.  workspace: device, 16-byte aligned; that of the largest call serves calls with fewer sequences and tokens. */
+/* One new token per sequence (generation): query s is sequence s's and sees all of its keys; tokens_q = sequences, causal and what
+ * q_start points to (it may be NULL) are not looked at.  workspace: device, 16-byte aligned; that of the largest call serves calls with fewer sequences and tokens. */
 size_t sl_attention_token_workspace_bytes(int64_t sequences, int64_t tokens_k, int heads, int kv_heads, int head_dim);
 int sl_attention_token(const sl_attention_shape *shape, const sl_heads *q, const sl_heads *k, const sl_heads *v, const sl_heads *out, void *workspace,
                        void *stream);
